@@ -61,6 +61,11 @@ extern "C" {
 #define ADAPT_ERR_HIP (-4)              /* a HIP runtime call or kernel launch failed */
 #define ADAPT_ERR_OUT_OF_MEMORY (-5)
 
+/* element types of the calls that take activations or gradients in more than one type */
+#define ADAPT_F32 0
+#define ADAPT_F16 1
+#define ADAPT_BF16 2
+
 /* thread-local text of the most recent error on this thread ("" if none); static storage */
 const char *adapt_last_error(void);
 
@@ -509,6 +514,75 @@ int adapt_relu_backward_f32(const float *dy_dev, const float *y_dev, float *dx_d
  * w_dev, g_dev: n floats each on the device, distinct; in place on w_dev.  Asynchronous on `stream`.
  * Errors: ADAPT_ERR_INVALID_ARGUMENT (NULL pointer, w_dev == g_dev), ADAPT_ERR_HIP. */
 int adapt_sgd_step_f32(float *w_dev, const float *g_dev, size_t n, float lr, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Token-wise operators: the exact 8-bit product that a table product is measured against, with a scale for every token and
+ * every output channel, its gradients, and the two layers around a recurrent text network that are no products: the
+ * embedding and dropout.  Activations and gradients come in the element type the call names (ADAPT_F32, ADAPT_F16,
+ * ADAPT_BF16), aligned to their elements; every sum and every step is held in 32 bits (integers, fp32) and rounded to
+ * the element type once, to nearest even.  Where a result is a sum of floats its order depends on the sizes alone: the same
+ * call gives the same bits.  All calls are asynchronous on `stream`, allocate nothing and may be recorded into a HIP
+ * graph; what they need beyond operands and results is a workspace of the caller's (aligned to 256 bytes, contents undefined
+ * afterwards, not shared by calls that may overlap in time).  Errors: ADAPT_ERR_INVALID_ARGUMENT (NULL or misaligned pointer, unknown
+ * element type, negative size, a result that is an operand, workspace too small or misaligned), ADAPT_ERR_UNSUPPORTED (the limits stated),
+ * ADAPT_ERR_HIP.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* Quantiser of Sec. III-A with the range taken from every row ("token") of x [tokens][cols] itself:
+ *     scales[t] = max_c |x[t][c]| / Q  (NaN skipped; 0 for a row of zeros or no columns),   Q = 2^(bits-1) - 1,
+ *     q[t][c] = clamp(round_half_even(x[t][c] / scales[t]), -Q, Q);   0 where x is NaN and where scales[t] = 0
+ * in fp32 (IEEE divisions), 2 <= bits <= 8.  A row that holds an infinity gets scales[t] = inf and codes 0: its products with
+ * adapt_int8_linear are NaN.  q_dev [tokens][cols] int8, scales_dev [tokens] fp32. */
+int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *scales_dev, size_t tokens, size_t cols, int bits,
+                          void *stream);
+
+/* Exact linear layer on int8 codes (all values -128 .. 127 are allowed):
+ *     acc[m][n] = sum_k a[m][k] * w[n][k]   (int32, exact: the sums of adapt_approx_linear with the table of the exact product)
+ *     y[m][n] = float(acc) * s_a[m] * s_w[n], then + bias[n] if bias_dev, then act (0 none, 1 y > 0 ? y : 0, 2 adapt_tanh_f32)
+ * left to right, every fp32 step rounded on its own.  a_dev [M][K], w_dev [N][K] int8; s_a_dev [M], s_w_dev [N], bias_dev [N]
+ * fp32; y_dev [M][N] of type y_type.  K = 0: sums of 0.  K <= 131071 (beyond, a sum may pass 32 bits) and M N < 2^36, else
+ * ADAPT_ERR_UNSUPPORTED. */
+int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev, const float *bias_dev, int act,
+                      void *y_dev, int y_type, int M, int K, int N, void *stream);
+
+/* Gradients of that layer without its activation, straight through both quantisers (Sec. III-A "Retraining"; a range taken from the
+ * row's own maximum clips nothing, so no gradient is masked):
+ *     dx[m][k] = sum_n (dy[m][n] * s_w[n]) * w[n][k]
+ *     dw[n][k] = sum_m (dy[m][n] * s_a[m]) * a[m][k]
+ *     db[n]    = sum_m dy[m][n]
+ * dy_dev [M][N], dx_dev [M][K], dw_dev [N][K], db_dev [N] of element type `type`; codes and scales as in adapt_int8_linear.  Any of dx_dev,
+ * dw_dev, db_dev may be NULL (not computed; a_dev and s_a_dev are read for dw alone, w_dev and s_w_dev for dx alone).  They are
+ * fully overwritten.  dy * s is formed in fp32 and kept to 24 bits (ADAPT_F32) or 16 bits (the 16-bit types, whose results keep 8 or 11).
+ * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
+ * dx_dev / dw_dev are given).  2^34 gradients or more in one matrix: ADAPT_ERR_UNSUPPORTED. */
+int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes);
+int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev,
+                               int M, int K, int N, void *dx_dev, void *dw_dev, void *db_dev, void *workspace_dev, size_t workspace_bytes,
+                               void *stream);
+
+/* Embedding: y[t] = table[tok[t]] * scale, rows of D elements of element type `type`; table_dev [V][D], y_dev [tokens][D].
+ * tokens_dev: int32 (token_bits 32) or int64 (64).  A token outside [0, V) gives a row of zeros.  At most 2^31 - 1 tokens. */
+int adapt_embedding(const void *table_dev, int type, const void *tokens_dev, int token_bits, void *y_dev, size_t tokens, int V, int D, float scale,
+                    void *stream);
+
+/* Its gradient: dtable[v] = scale * sum over the places t with tok[t] = v of dy[t]; rows of tokens that do not occur, and row
+ * padding_idx (-1: none), are zero; places whose token is padding_idx or lies outside [0, V) take no part (their dy is not read).
+ * dtable_dev [V][D] of dy's element type, fully overwritten.  The places are sorted by token, so no sum depends on an order of
+ * atomics.  workspace_dev: adapt_embedding_backward_workspace bytes. */
+int adapt_embedding_backward_workspace(size_t tokens, int V, int D, size_t *bytes);
+int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_dev, int token_bits, void *dtable_dev, size_t tokens, int V, int D, float scale,
+                             int64_t padding_idx, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Dropout, 0 <= p <= 1:  y[i] = kept(i) ? x[i] * (1 / (1 - p)) : 0, the factor rounded to fp32; a dropped element is 0 whatever x holds.
+ * The mask is computed, never stored: kept(i) = word i % 4 of the Philox4x32-10 block with counter (i / 4, offset + *step) (two 64-bit
+ * numbers, low word first) and key `seed` is at least p * 2^32 (rounded).  The same seed, offset and step give the same mask in either
+ * direction and for every element type.  step_dev: a device counter that is read when the kernel runs, or NULL for 0: a recorded graph draws a
+ * new mask at every replay if the program moves the counter on between replays.  The backward pass is the same map on dy.
+ * x_dev, y_dev: n elements; y_dev may be x_dev. */
+int adapt_dropout(const void *x_dev, void *y_dev, int type, size_t n, float p, uint64_t seed, uint64_t offset, const uint64_t *step_dev,
+                  void *stream);
+int adapt_dropout_backward(const void *dy_dev, void *dx_dev, int type, size_t n, float p, uint64_t seed, uint64_t offset, const uint64_t *step_dev,
+                           void *stream);
 
 #ifdef __cplusplus
 }

@@ -38,6 +38,8 @@ EXPORTS = [
     "adapt_approx_linear_i16", "adapt_approx_conv2d_i16", "adapt_approx_linear_func_i16", "adapt_approx_conv2d_func_i16",
     "adapt_linear_layer_i16_f32", "adapt_conv2d_layer_i16_f32",
     "adapt_ste_linear_backward_f32", "adapt_sgd_step_f32", "adapt_relu_backward_f32", "adapt_ste_conv2d_backward_workspace", "adapt_ste_conv2d_backward_f32",
+    "adapt_quantize_tokens", "adapt_int8_linear", "adapt_int8_linear_backward_workspace", "adapt_int8_linear_backward",
+    "adapt_embedding", "adapt_embedding_backward_workspace", "adapt_embedding_backward", "adapt_dropout", "adapt_dropout_backward",
 ]
 
 
@@ -125,6 +127,16 @@ def load() -> ctypes.CDLL:
     L.adapt_relu_backward_f32.argtypes = [vp, vp, vp, sz, vp]
     L.adapt_ste_conv2d_backward_workspace.argtypes = [i32] * 15 + [ctypes.POINTER(sz)]
     L.adapt_ste_conv2d_backward_f32.argtypes = [vp, vp, vp] + [i32] * 13 + [f32, f32, i32, vp, vp, vp, vp, sz, vp]
+    i64, u64 = ctypes.c_int64, ctypes.c_uint64
+    L.adapt_quantize_tokens.argtypes = [vp, i32, vp, vp, sz, sz, i32, vp]
+    L.adapt_int8_linear.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, vp]
+    L.adapt_int8_linear_backward_workspace.argtypes = [i32] * 6 + [ctypes.POINTER(sz)]
+    L.adapt_int8_linear_backward.argtypes = [vp, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    L.adapt_embedding.argtypes = [vp, i32, vp, i32, vp, sz, i32, i32, f32, vp]
+    L.adapt_embedding_backward_workspace.argtypes = [sz, i32, i32, ctypes.POINTER(sz)]
+    L.adapt_embedding_backward.argtypes = [vp, i32, vp, i32, vp, sz, i32, i32, f32, i64, vp, sz, vp]
+    L.adapt_dropout.argtypes = [vp, vp, i32, sz, f32, u64, u64, vp, vp]
+    L.adapt_dropout_backward.argtypes = [vp, vp, i32, sz, f32, u64, u64, vp, vp]
     L.adapt_ste_linear_backward_f32.argtypes = [vp, vp, vp, i32, i32, i32, f32, f32, i32, vp, vp, vp, vp]
     for name in EXPORTS:
         if name != "adapt_last_error":
@@ -832,3 +844,157 @@ def adapt_relu_backward_f32(dy, y, out=None, stream=None):
         out = torch.empty_like(dy)
     _chk(load().adapt_relu_backward_f32(_ptr(dy, torch.float32), _ptr(y, torch.float32), _ptr(out, torch.float32), dy.numel(), _stream(stream)))
     return out
+
+
+# ---- token-wise operators: element types, and results in memory of the stream the call runs on
+
+ELEMENT_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+def _element(t):
+    if t.dtype not in ELEMENT_TYPES:
+        raise TypeError(f"expected float32, float16 or bfloat16, got {t.dtype}")
+    return ELEMENT_TYPES[t.dtype]
+
+
+def _shape(what, t, want):
+    if tuple(t.shape) != tuple(want):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(want)}")
+
+
+def _here(*tensors):
+    """The library launches on the current device: tensors of another one would be read from the wrong side."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != here:
+            raise ValueError(f"tensor on cuda:{t.device.index}, but the current device is cuda:{here}")
+
+
+def _new(stream, shape, dtype):
+    """Memory of `stream` (a block given back on the current stream may still be in use there)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _workspace(workspace, need, stream):
+    """The caller's uint8 tensor if it is large enough, else a new one that lives until the call's kernels have run."""
+    if need == 0:
+        return None, 0
+    if workspace is None or workspace.numel() < need:
+        workspace = _new(stream, (need,), torch.uint8)
+    return ctypes.c_void_p(_ptr(workspace, torch.uint8)), workspace.numel()
+
+
+def adapt_quantize_tokens(x, bits: int = 8, out=None, scales=None, stream=None):
+    """x [tokens][cols] -> (int8 codes [tokens][cols], fp32 scale per token)."""
+    tokens, cols = x.shape
+    _here(x, out, scales)
+    if out is None:
+        out = _new(stream, (tokens, cols), torch.int8)
+    if scales is None:
+        scales = _new(stream, (tokens,), torch.float32)
+    _shape("out", out, (tokens, cols))
+    _shape("scales", scales, (tokens,))
+    _chk(load().adapt_quantize_tokens(_ptr(x), _element(x), _ptr(out, torch.int8), _ptr(scales, torch.float32), tokens, cols, bits,
+                                      _stream(stream)))
+    return out, scales
+
+
+def adapt_int8_linear(a, s_a, w, s_w, bias=None, act: int = 0, dtype=torch.float32, out=None, stream=None):
+    """Codes a [M][K], w [N][K] with scales s_a [M], s_w [N] -> act(a w^T s_a s_w + bias) [M][N] of `dtype` (out's, if given)."""
+    M, K = a.shape
+    N = w.shape[0]
+    _shape("w", w, (N, K))
+    _shape("s_a", s_a, (M,))
+    _shape("s_w", s_w, (N,))
+    if bias is not None:
+        _shape("bias", bias, (N,))
+    _here(a, s_a, w, s_w, bias, out)
+    if out is None:
+        out = _new(stream, (M, N), dtype)
+    _shape("out", out, (M, N))
+    _chk(load().adapt_int8_linear(_ptr(a, torch.int8), _ptr(s_a, torch.float32), _ptr(w, torch.int8), _ptr(s_w, torch.float32),
+                                  _ptr(bias, torch.float32), act, _ptr(out), _element(out), M, K, N, _stream(stream)))
+    return out
+
+
+def adapt_int8_linear_backward(dy, a, s_a, w, s_w, want=("dx", "dw", "db"), workspace=None, stream=None):
+    """dy [M][N] and the operands of the forward pass -> (dx [M][K], dw [N][K], db [N]) of dy's type; entries not in `want` are None.
+    workspace: a uint8 device tensor to reuse (allocated here when None or too small)."""
+    M, N = dy.shape
+    K = w.shape[1]
+    _shape("a", a, (M, K))
+    _shape("w", w, (N, K))
+    _shape("s_a", s_a, (M,))
+    _shape("s_w", s_w, (N,))
+    _here(dy, a, s_a, w, s_w, workspace)
+    need = ctypes.c_size_t(0)
+    _chk(load().adapt_int8_linear_backward_workspace(M, K, N, _element(dy), int("dx" in want), int("dw" in want), ctypes.byref(need)))
+    ws, ws_bytes = _workspace(workspace, need.value, stream)
+    dx = _new(stream, (M, K), dy.dtype) if "dx" in want else None
+    dw = _new(stream, (N, K), dy.dtype) if "dw" in want else None
+    db = _new(stream, (N,), dy.dtype) if "db" in want else None
+    _chk(load().adapt_int8_linear_backward(_ptr(dy), _element(dy), _ptr(a, torch.int8), _ptr(s_a, torch.float32), _ptr(w, torch.int8),
+                                           _ptr(s_w, torch.float32), M, K, N, _ptr(dx), _ptr(dw), _ptr(db), ws, ws_bytes, _stream(stream)))
+    return dx, dw, db
+
+
+def _tokens(tokens):
+    if tokens.dtype not in TOKEN_BITS:
+        raise TypeError(f"expected int32 or int64 tokens, got {tokens.dtype}")
+    return _ptr(tokens), TOKEN_BITS[tokens.dtype]
+
+
+def adapt_embedding(table, tokens, scale: float = 1.0, out=None, stream=None):
+    """Rows of table [V][D] for tokens of any shape, times scale; a token outside [0, V) gives zeros."""
+    V, D = table.shape
+    _here(table, tokens, out)
+    if out is None:
+        out = _new(stream, tuple(tokens.shape) + (D,), table.dtype)
+    _shape("out", out, tuple(tokens.shape) + (D,))
+    tok, tok_bits = _tokens(tokens)
+    _chk(load().adapt_embedding(_ptr(table), _element(table), tok, tok_bits, _ptr(out, table.dtype), tokens.numel(), V, D, float(scale), _stream(stream)))
+    return out
+
+
+def adapt_embedding_backward(dy, tokens, V: int, scale: float = 1.0, padding_idx: int = -1, out=None, workspace=None, stream=None):
+    """dy [...][D] at tokens [...] -> gradient [V][D] of the table, of dy's type.
+    workspace: a uint8 device tensor to reuse (allocated here when None or too small)."""
+    D = dy.shape[-1]
+    _shape("dy", dy, tuple(tokens.shape) + (D,))
+    _here(dy, tokens, out, workspace)
+    if out is None:
+        out = _new(stream, (V, D), dy.dtype)
+    _shape("out", out, (V, D))
+    need = ctypes.c_size_t(0)
+    _chk(load().adapt_embedding_backward_workspace(tokens.numel(), V, D, ctypes.byref(need)))
+    ws, ws_bytes = _workspace(workspace, need.value, stream)
+    tok, tok_bits = _tokens(tokens)
+    _chk(load().adapt_embedding_backward(_ptr(dy), _element(dy), tok, tok_bits, _ptr(out, dy.dtype), tokens.numel(), V, D, float(scale), padding_idx, ws,
+                                         ws_bytes, _stream(stream)))
+    return out
+
+
+def _dropout(call, x, p, seed, offset, step, out, stream):
+    _here(x, step, out)
+    if out is None:
+        out = _new(stream, tuple(x.shape), x.dtype)
+    _shape("out", out, tuple(x.shape))
+    if step is not None and step.numel() != 1:
+        raise ValueError("step must hold one int64")
+    _chk(call(_ptr(x), _ptr(out, x.dtype), _element(x), x.numel(), float(p), int(seed), int(offset), _ptr(step, torch.int64), _stream(stream)))
+    return out
+
+
+def adapt_dropout(x, p: float, seed: int, offset: int = 0, step=None, out=None, stream=None):
+    """x with a share p of its elements set to 0 and the others times 1 / (1 - p); the mask is that of (seed, offset + step).
+    step: a one-element int64 device tensor that the kernel reads, or None.  out may be x."""
+    return _dropout(load().adapt_dropout, x, p, seed, offset, step, out, stream)
+
+
+def adapt_dropout_backward(dy, p: float, seed: int, offset: int = 0, step=None, out=None, stream=None):
+    """The gradient through adapt_dropout with the same seed, offset and step.  out may be dy."""
+    return _dropout(load().adapt_dropout_backward, dy, p, seed, offset, step, out, stream)

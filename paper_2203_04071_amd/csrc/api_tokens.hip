@@ -1,0 +1,292 @@
+// C ABI, part 5: the exact 8-bit product with a scale for each token and channel and its gradients, embedding, dropout.
+#include <cmath>
+
+#include "api_common.hpp"
+#include "dropout.hpp"
+#include "embedding.hpp"
+#include "int8_linear.hpp"
+#include "quantize_tokens.hpp"
+
+using namespace adapt_api;
+
+namespace {
+
+bool off_by(const void *p, size_t align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Tiles of a product: a launch is limited to 2^32 threads, 2^24 workgroups of 256.
+constexpr long long INT8_TILES = 1ll << 24;
+
+constexpr int INT8_MAX_K = 131071;      // (-128)^2 K < 2^31
+
+int int8_args(const char *who, int M, int K, int N, int type) {
+    if (M < 0 || K < 0 || N < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
+    if (!adapt::element_size(type)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
+    return ADAPT_OK;
+}
+
+struct EmbedPlan {
+    uint32_t T, V, D, C, pieces, blocks;
+    int passes, bits;
+    size_t keys, counts, used, part, bytes;     // offsets of the regions (keys at 0: two pairs of T)
+};
+EmbedPlan embed_plan(size_t T, int V, int D) {
+    EmbedPlan e{};
+    e.T = (uint32_t)T;
+    e.V = (uint32_t)V;
+    e.D = (uint32_t)D;
+    e.C = 32;
+    e.pieces = (e.T + e.C - 1) / e.C;
+    e.blocks = (e.T + adapt::EMB_TILE - 1) / adapt::EMB_TILE;
+    int b = 1;
+    while ((e.V >> b) != 0) ++b;                // keys 0 .. V
+    e.passes = (b + adapt::EMB_BITS - 1) / adapt::EMB_BITS;
+    e.bits = (b + e.passes - 1) / e.passes;
+    const size_t list = round256((size_t)e.T * 4);
+    e.counts = 4 * list;
+    e.used = e.counts + round256(((size_t)e.blocks << e.bits) * 4);
+    e.part = e.used + round256((size_t)e.V);
+    e.bytes = e.part + 2 * round256((size_t)e.pieces * e.D * 4);
+    return e;
+}
+
+int embed_args(const char *who, size_t T, int V, int D) {
+    if (V < 0 || D < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
+    if (T >= (1ull << 31)) return fail(ADAPT_ERR_UNSUPPORTED, "%s: more than 2^31-1 tokens", who);
+    return ADAPT_OK;
+}
+
+// lanes that share a row of D elements in 16-byte pieces: 2^lg of them, at most a workgroup
+template <typename E>
+int lanes_lg(int D) {
+    int lg = 0;
+    while (lg < 8 && ((long long)adapt::piece_len<E> << lg) < D) ++lg;
+    return lg;
+}
+
+unsigned cap_grid(size_t g, size_t cap) { return (unsigned)(g < 1 ? 1 : (g > cap ? cap : g)); }
+
+template <typename Tok>
+void embed_sort(const EmbedPlan &e, const Tok *tokens, char *ws, int64_t padding, hipStream_t s, const uint32_t **key, const uint32_t **at) {
+    const size_t list = round256((size_t)e.T * 4);
+    adapt::EmbedSort p{};
+    p.counts = reinterpret_cast<uint32_t *>(ws + e.counts);
+    p.used = reinterpret_cast<uint8_t *>(ws + e.used);
+    p.T = e.T;
+    p.V = e.V;
+    p.bits = e.bits;
+    p.padding = padding;
+    for (int pass = 0; pass < e.passes; ++pass) {
+        char *const to = ws + (pass & 1 ? 2 * list : 0);
+        p.key_out = reinterpret_cast<uint32_t *>(to);
+        p.at_out = reinterpret_cast<uint32_t *>(to + list);
+        p.shift = pass * e.bits;
+        adapt::embed_count_kernel<<<e.blocks, adapt::EMB_THREADS, 0, s>>>(p, tokens);
+        adapt::embed_scan_kernel<<<1, 1024, 0, s>>>(p.counts, e.blocks << e.bits);
+        adapt::embed_scatter_kernel<<<e.blocks, adapt::EMB_THREADS, 0, s>>>(p, tokens);
+        p.key_in = p.key_out;
+        p.at_in = p.at_out;
+    }
+    *key = p.key_in;
+    *at = p.at_in;
+}
+
+int dropout(const char *who, const void *x_dev, void *y_dev, int type, size_t n, float p, uint64_t seed, uint64_t offset, const uint64_t *step_dev, void *stream) {
+    const size_t e = (size_t)adapt::element_size(type);
+    if (!e) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
+    if (!(p >= 0.0f && p <= 1.0f)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: p must be in [0,1]", who);
+    if (!n) return ADAPT_OK;
+    if (!x_dev || !y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
+    if (off_by(x_dev, e) || off_by(y_dev, e) || off_by(step_dev, 8)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    adapt::DropoutParams q{};
+    q.seed = seed;
+    q.offset = offset;
+    q.step = step_dev;
+    const double thr = std::nearbyint((double)p * 4294967296.0);
+    q.none = thr >= 4294967296.0;
+    q.threshold = q.none ? 0xffffffffu : (uint32_t)thr;
+    q.scale = q.none ? 0.0f : (float)(1.0 / (1.0 - (double)p));
+    q.n = n;
+    const unsigned grid = cap_grid((n + 4 * adapt::DROP_THREADS - 1) / (4 * adapt::DROP_THREADS), 256 * 16);
+    ADAPT_FOR_TYPE(type, E, adapt::dropout_kernel<E><<<grid, adapt::DROP_THREADS, 0, (hipStream_t)stream>>>(
+                                static_cast<const E::mem *>(x_dev), static_cast<E::mem *>(y_dev), q));
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *scales_dev, size_t tokens, size_t cols, int bits, void *stream) {
+    const char *who = "adapt_quantize_tokens";
+    const size_t e = (size_t)adapt::element_size(x_type);
+    if (!e) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, x_type);
+    if (bits < 2 || bits > 8) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bits=%d not in [2,8]", who, bits);
+    if (!tokens) return ADAPT_OK;
+    if (!scales_dev || (cols && (!x_dev || !q_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
+    if (off_by(x_dev, e) || off_by(scales_dev, 4)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (cols && x_dev == (const void *)q_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
+    const float Q = (float)((1 << (bits - 1)) - 1);
+    const unsigned grid = cap_grid(tokens, 1u << 20);
+    ADAPT_FOR_TYPE(x_type, E, adapt::quantize_tokens_kernel<E><<<grid, adapt::QT_THREADS, 0, (hipStream_t)stream>>>(
+                                  static_cast<const E::mem *>(x_dev), q_dev, scales_dev, tokens, cols, Q));
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev, const float *bias_dev, int act,
+                      void *y_dev, int y_type, int M, int K, int N, void *stream) {
+    const char *who = "adapt_int8_linear";
+    if (int rc = int8_args(who, M, K, N, y_type)) return rc;
+    if (act < 0 || act > 2) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: act=%d not in [0,2]", who, act);
+    if (!M || !N) return ADAPT_OK;
+    if (!s_a_dev || !s_w_dev || !y_dev || (K && (!a_dev || !w_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
+    if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4) || off_by(bias_dev, 4) || off_by(y_dev, (size_t)adapt::element_size(y_type)))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (K > INT8_MAX_K) return fail(ADAPT_ERR_UNSUPPORTED, "%s: K=%d above %d, sums could pass 32 bits", who, K, INT8_MAX_K);
+    const long long tiles = (((long long)M + 63) / 64) * (((long long)N + 63) / 64);
+    if (tiles >= INT8_TILES) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^36 outputs or more", who);
+    const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, bias_dev, y_dev, M, K, N, act};
+    ADAPT_FOR_TYPE(y_type, E, adapt::int8_linear_kernel<E><<<(unsigned)tiles, 256, 0, (hipStream_t)stream>>>(p));
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes) {
+    const char *who = "adapt_int8_linear_backward_workspace";
+    if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
+    *bytes = 0;
+    if (int rc = int8_args(who, M, K, N, type)) return rc;
+    return ADAPT_OK;
+}
+
+int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev,
+                               int M, int K, int N, void *dx_dev, void *dw_dev, void *db_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
+    const char *who = "adapt_int8_linear_backward";
+    if (int rc = int8_args(who, M, K, N, type)) return rc;
+    const size_t e = (size_t)adapt::element_size(type);
+    const bool want_dx = dx_dev && M > 0 && K > 0, want_dw = dw_dev && N > 0 && K > 0, want_db = db_dev && N > 0;
+    if (!want_dx && !want_dw && !want_db) return ADAPT_OK;
+    if (M > 0 && N > 0 && !dy_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL dy_dev", who);
+    if (want_dx && N > 0 && (!w_dev || !s_w_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL w_dev / s_w_dev", who);
+    if (want_dw && M > 0 && (!a_dev || !s_a_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL a_dev / s_a_dev", who);
+    for (const void *q : {dy_dev, (const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
+        if (off_by(q, e)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    for (const void *g : {(const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
+        if (g && (g == dy_dev || g == (const void *)a_dev || g == (const void *)w_dev))
+            return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
+    size_t need = 0;
+    if (int rc = adapt_int8_linear_backward_workspace(M, K, N, type, want_dx, want_dw, &need)) return rc;
+    if (need && (!workspace_dev || workspace_bytes < need || off_by(workspace_dev, 256)))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, need);
+    const long long tx = (((long long)M + 31) / 32) * (((long long)K + 31) / 32), tw = (((long long)N + 31) / 32) * (((long long)K + 31) / 32);
+    if ((want_dx && tx >= INT8_TILES) || (want_dw && tw >= INT8_TILES)) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^34 gradients or more", who);
+    hipStream_t s = (hipStream_t)stream;
+    ADAPT_FOR_TYPE(type, E, {
+        const E::mem *const dy = static_cast<const E::mem *>(dy_dev);
+        if (want_dx) adapt::int8_gradient_kernel<E><<<(unsigned)tx, 256, 0, s>>>(dy, (size_t)N, 1, s_w_dev, w_dev, static_cast<E::mem *>(dx_dev), M, K, N);
+        if (want_dw) adapt::int8_gradient_kernel<E><<<(unsigned)tw, 256, 0, s>>>(dy, 1, (size_t)N, s_a_dev, a_dev, static_cast<E::mem *>(dw_dev), N, K, M);
+        if (want_db) adapt::int8_bias_grad_kernel<E><<<(unsigned)((N + 31ll) / 32), 256, 0, s>>>(dy, static_cast<E::mem *>(db_dev), M, N);
+    });
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+/* ------------------------------------------------------------------ embedding */
+
+int adapt_embedding(const void *table_dev, int type, const void *tokens_dev, int token_bits, void *y_dev, size_t tokens, int V, int D, float scale,
+                    void *stream) {
+    const char *who = "adapt_embedding";
+    const size_t e = (size_t)adapt::element_size(type);
+    if (!e) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
+    if (token_bits != 32 && token_bits != 64) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: token_bits=%d is neither 32 nor 64", who, token_bits);
+    if (int rc = embed_args(who, tokens, V, D)) return rc;
+    if (!tokens || !D) return ADAPT_OK;
+    if (!tokens_dev || !y_dev || (V && !table_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
+    if (off_by(table_dev, e) || off_by(y_dev, e) || off_by(tokens_dev, (size_t)token_bits / 8))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (table_dev == y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
+    hipStream_t s = (hipStream_t)stream;
+    ADAPT_FOR_TYPE(type, E, {
+        const int lg = lanes_lg<E>(D);
+        const unsigned grid = cap_grid((tokens + (adapt::EMB_THREADS >> lg) - 1) / (adapt::EMB_THREADS >> lg), 1u << 16);
+        const E::mem *const table = static_cast<const E::mem *>(table_dev);
+        if (token_bits == 64)
+            adapt::embedding_kernel<E, int64_t><<<grid, adapt::EMB_THREADS, 0, s>>>(table, static_cast<const int64_t *>(tokens_dev), static_cast<E::mem *>(y_dev),
+                                                                                  tokens, (uint32_t)V, (uint32_t)D, scale, lg);
+        else
+            adapt::embedding_kernel<E, int32_t><<<grid, adapt::EMB_THREADS, 0, s>>>(table, static_cast<const int32_t *>(tokens_dev), static_cast<E::mem *>(y_dev),
+                                                                                  tokens, (uint32_t)V, (uint32_t)D, scale, lg);
+    });
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+int adapt_embedding_backward_workspace(size_t tokens, int V, int D, size_t *bytes) {
+    const char *who = "adapt_embedding_backward_workspace";
+    if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
+    *bytes = 0;
+    if (int rc = embed_args(who, tokens, V, D)) return rc;
+    *bytes = embed_plan(tokens, V, D).bytes;
+    return ADAPT_OK;
+}
+
+int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_dev, int token_bits, void *dtable_dev, size_t tokens, int V, int D, float scale,
+                             int64_t padding_idx, void *workspace_dev, size_t workspace_bytes, void *stream) {
+    const char *who = "adapt_embedding_backward";
+    const size_t e = (size_t)adapt::element_size(type);
+    if (!e) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
+    if (token_bits != 32 && token_bits != 64) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: token_bits=%d is neither 32 nor 64", who, token_bits);
+    if (int rc = embed_args(who, tokens, V, D)) return rc;
+    if (!V || !D) return ADAPT_OK;
+    if (!dtable_dev || (tokens && (!tokens_dev || !dy_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
+    if (off_by(dy_dev, e) || off_by(dtable_dev, e) || off_by(tokens_dev, (size_t)token_bits / 8))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (dy_dev == dtable_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: the gradient must not alias an input", who);
+    const EmbedPlan pl = embed_plan(tokens, V, D);
+    if (!workspace_dev || workspace_bytes < pl.bytes || off_by(workspace_dev, 256))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, pl.bytes);
+    hipStream_t s = (hipStream_t)stream;
+    char *const ws = static_cast<char *>(workspace_dev);
+    adapt::fill_u32_kernel<<<ew_grid(((size_t)V + 3) / 4), adapt::EW_THREADS, 0, s>>>(reinterpret_cast<uint32_t *>(ws + pl.used), 0u, ((size_t)V + 3) / 4);
+    adapt::EmbedSum p{};
+    if (tokens) {
+        if (token_bits == 64) embed_sort(pl, static_cast<const int64_t *>(tokens_dev), ws, padding_idx, s, &p.key, &p.at);
+        else embed_sort(pl, static_cast<const int32_t *>(tokens_dev), ws, padding_idx, s, &p.key, &p.at);
+    }
+    p.used = reinterpret_cast<uint8_t *>(ws + pl.used);
+    p.head = reinterpret_cast<float *>(ws + pl.part);
+    p.tail = reinterpret_cast<float *>(ws + pl.part + round256((size_t)pl.pieces * pl.D * 4));
+    p.T = pl.T;
+    p.V = pl.V;
+    p.D = pl.D;
+    p.C = pl.C;
+    p.pieces = pl.pieces;
+    p.scale = scale;
+    ADAPT_FOR_TYPE(type, E, {
+        p.lg = lanes_lg<E>(D);
+        const unsigned per = (unsigned)(adapt::EMB_THREADS >> p.lg);
+        p.sum_blocks = (pl.pieces + per - 1) / per;
+        const unsigned zero_blocks = cap_grid(((size_t)V + per - 1) / per, 2048);
+        adapt::embed_sum_kernel<E><<<p.sum_blocks + zero_blocks, adapt::EMB_THREADS, 0, s>>>(p, static_cast<const E::mem *>(dy_dev), static_cast<E::mem *>(dtable_dev));
+        if (pl.pieces > 1) adapt::embed_join_kernel<E><<<pl.pieces - 1, adapt::EMB_THREADS, 0, s>>>(p, static_cast<E::mem *>(dtable_dev));
+    });
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+/* ------------------------------------------------------------------ dropout */
+
+int adapt_dropout(const void *x_dev, void *y_dev, int type, size_t n, float p, uint64_t seed, uint64_t offset, const uint64_t *step_dev, void *stream) {
+    return dropout("adapt_dropout", x_dev, y_dev, type, n, p, seed, offset, step_dev, stream);
+}
+
+int adapt_dropout_backward(const void *dy_dev, void *dx_dev, int type, size_t n, float p, uint64_t seed, uint64_t offset, const uint64_t *step_dev,
+                           void *stream) {
+    return dropout("adapt_dropout_backward", dy_dev, dx_dev, type, n, p, seed, offset, step_dev, stream);
+}
+
+}  // extern "C"

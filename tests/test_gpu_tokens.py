@@ -1,0 +1,558 @@
+"""Token-wise operators on the GPU against the oracle: exact 8-bit product with token and channel scales, its quantiser and gradients,
+embedding and its gradient, dropout.
+
+Tolerances.  Steps that the header orders one by one (quantiser, product with its finish, lookup, dropout) are compared bit for bit:
+the oracle takes the same fp32 steps, and the last rounding to fp16 / bf16 is the nearest one.  Sums of floats are compared with sums in
+64 bits: with u = 2^-24, fp32 sums of R terms in any order are within (R + 2) u * sum |term| (a rounding per addition, two to form
+a term), a 16-bit result adds half a step of its type (eps / 2 of the value, or half of its smallest subnormal), and a gradient
+of the product on a 16-bit type keeps 16 bits of dy * s: 2^-17 * sum |term| more."""
+import numpy as np
+import pytest
+
+import oracle as orc
+from oracle import tokens as ot
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ("f32", "f16", "bf16")
+U = 2.0 ** -24
+
+
+def _t(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2203_04071_amd import binding
+    return binding
+
+
+def dev(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t.to(dtype) if dtype is not None else t).cuda()
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def rounded(x32, name):
+    """fp32 numpy -> the nearest values of the type, as a CPU tensor"""
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x32, dtype=np.float32)).to(_t(name))
+
+
+def same_bits(got, want):
+    import torch
+    got = got.detach().cpu()
+    assert got.dtype == want.dtype and got.shape == want.shape
+    g, w = got.float().numpy(), want.float().numpy()
+    ok = (g == w) | (np.isnan(g) & np.isnan(w))
+    assert ok.all(), (int((~ok).sum()), got.shape, np.argwhere(~ok)[:4].tolist(), g[~ok][:4], w[~ok][:4])
+
+
+def within(got, want, mass, terms, name, kept=0.0):
+    """|got - want| <= bound of the module text; mass: sum of |terms|"""
+    import torch
+    fi = torch.finfo(_t(name))
+    got = f64(got)
+    bound = ((terms + 2) * U + kept) * mass + 2.0 ** -149 * (terms + 2)
+    if name != "f32":
+        bound = bound * (1 + fi.eps) + fi.eps / 2 * np.abs(want) + fi.smallest_normal * fi.eps / 2
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4], np.broadcast_to(bound, got.shape)[bad][:4])
+
+
+def randn(rng, shape, name):
+    """Values of the type, as the fp32 numpy array that holds them and the device tensor"""
+    t = rounded(rng.standard_normal(shape).astype(np.float32), name)
+    return t.float().numpy(), t.cuda()
+
+
+# ---------------------------------------------------------------------------------------------- quantiser
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,bits", [(1, 1, 8), (3, 7, 8), (1, 512, 8), (5, 63, 4), (4, 64, 2), (9, 65, 8), (33, 1000, 8), (6, 1024, 6), (7, 1025, 8),
+                                      (5, 2048, 8), (3, 2049, 7), (4, 4097, 8), (3, 8192, 8), (2, 8193, 8), (2, 16384, 8), (2, 16385, 8), (2, 40001, 8),
+                                      (3000, 24, 8)])
+def test_quantize_tokens(B, name, M, K, bits):
+    rng = np.random.default_rng(M * 100003 + K)
+    x, xd = randn(rng, (M, K), name)
+    q, s = B.adapt_quantize_tokens(xd, bits)
+    wq, ws = ot.quantize_tokens(x, bits)
+    assert (s.cpu().numpy() == ws).all()
+    assert (q.cpu().numpy() == wq).all()
+
+
+@pytest.mark.parametrize("K", [40, 700, 1500, 3000, 9000, 20000])
+@pytest.mark.parametrize("name", TYPES)
+def test_quantize_tokens_special_rows(B, name, K):
+    """Rows of zeros, NaN, infinities, subnormal ranges, ties, the largest numbers; what lies behind the results stays."""
+    import torch
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal((12, K)).astype(np.float32)
+    x[0] = 0
+    x[1, :] = np.nan
+    x[2, 3] = np.nan
+    x[3, K - 1] = np.inf
+    x[4, 0] = -np.inf
+    x[5] *= 1e-44           # range / 127 rounds to 0 or to a subnormal with few bits
+    x[6] *= 1e-39
+    x[7] = np.where(np.arange(K) % 2 == 0, 127.0, (np.arange(K) % 250) / 2.0)      # ties: halves of the scale 1
+    x[8] = 3.0e38
+    x[9] = -0.0
+    x[10, 1:] = 0
+    with np.errstate(over="ignore"):
+        t = rounded(x, name)
+    x = t.float().numpy()
+    q = torch.full((13, K), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((13,), 7.0, device="cuda")
+    B.adapt_quantize_tokens(t.cuda(), 8, out=q[:12], scales=s[:12])
+    wq, ws = ot.quantize_tokens(x, 8)
+    assert np.array_equal(s.cpu().numpy()[:12], ws)
+    assert (q.cpu().numpy()[:12] == wq).all()
+    assert (q[12] == 99).all() and s[12] == 7.0
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("K", [129, 1023, 5001])
+def test_quantize_tokens_at_odd_addresses(B, name, K):
+    """Rows that start at an element's own alignment, codes at any byte."""
+    import torch
+    rng = np.random.default_rng(K)
+    x, _ = randn(rng, (5, K), name)
+    flat = torch.zeros(5 * K + 1, dtype=_t(name), device="cuda")
+    flat[1:] = rounded(x, name).cuda().view(-1)
+    q = torch.zeros(5 * K + 3, dtype=torch.int8, device="cuda")
+    B.adapt_quantize_tokens(flat[1:].view(5, K), 8, out=q[3:].view(5, K))
+    assert (q[3:].view(5, K).cpu().numpy() == ot.quantize_tokens(x, 8)[0]).all() and (q[:3] == 0).all()
+
+
+def test_quantize_tokens_without_columns(B):
+    import torch
+    s = torch.full((3,), 5.0, device="cuda")
+    B.adapt_quantize_tokens(torch.empty((3, 0), device="cuda"), 8, scales=s)
+    assert (s == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------- product
+
+def codes(rng, rows, cols):
+    return rng.integers(-128, 128, (rows, cols), dtype=np.int8)
+
+
+def scales(rng, n):
+    return (rng.uniform(0.5, 2.0, n) * 0.01).astype(np.float32)
+
+
+PRODUCTS = [(1, 1, 1), (1, 512, 2048), (1, 16, 8), (2, 31, 3), (3, 33, 65), (1, 777, 999), (5, 64, 17), (8, 4096, 80), (16, 128, 16), (17, 100, 130),
+            (33, 1000, 100), (31, 15, 31), (32, 32, 32), (64, 64, 64), (65, 48, 63), (63, 80, 129), (100, 144, 100), (128, 128, 128), (129, 127, 257),
+            (200, 4112, 72), (256, 256, 256), (257, 272, 255), (300, 1, 300), (300, 17, 40), (7, 1040, 300), (512, 512, 512), (640, 96, 1000), (1111, 777, 99),
+            (1, 16384, 40), (4, 5000, 24), (24, 2000, 48), (48, 3001, 33)]
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", PRODUCTS)
+def test_int8_linear(B, name, M, K, N):
+    rng = np.random.default_rng(M * 7 + K * 1009 + N)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    bias = rng.standard_normal(N).astype(np.float32)
+    ad, wd, sad, swd = dev(a), dev(w), dev(s_a), dev(s_w)
+    same_bits(B.adapt_int8_linear(ad, sad, wd, swd, dtype=_t(name)), rounded(ot.int8_linear(a, s_a, w, s_w), name))
+    same_bits(B.adapt_int8_linear(ad, sad, wd, swd, bias=dev(bias), act=1, dtype=_t(name)), rounded(ot.int8_linear(a, s_a, w, s_w, bias, 1), name))
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 512, 64), (40, 300, 70), (300, 256, 300)])
+def test_int8_linear_tanh_and_scales_as_they_come(B, M, K, N):
+    """tanh is the library's own; scales of zero, infinity and NaN go through the formula."""
+    rng = np.random.default_rng(8)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N) * 0.1
+    bias = rng.standard_normal(N).astype(np.float32)
+    got = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), bias=dev(bias), act=2)
+    same_bits(got, rounded(ot.int8_linear(a, s_a, w, s_w, bias, 2, tanh=orc.tanh), "f32"))
+    s_w[[0, 5, 9, 20]] = 0.0, np.inf, np.nan, 1e-42
+    s_a[0] = np.inf if M > 1 else 1e30
+    same_bits(B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w)), rounded(ot.int8_linear(a, s_a, w, s_w), "f32"))
+
+
+@pytest.mark.parametrize("M,N", [(1, 3), (70, 64), (256, 300)])
+@pytest.mark.parametrize("value", [-128, 127])
+def test_int8_linear_longest_sums(B, M, N, value):
+    """The largest inner dimension with every product at its extreme: the sum fits 32 bits exactly; odd lengths below it."""
+    for K in (131071, 131056):
+        a = np.full((M, K), -128, np.int8)
+        w = np.full((N, K), value, np.int8)
+        one, ones = np.ones(M, np.float32), np.ones(N, np.float32)
+        got = B.adapt_int8_linear(dev(a), dev(one), dev(w), dev(ones))
+        assert (f64(got) == np.float32(-128 * value * K)).all()
+
+
+@pytest.mark.parametrize("M,N", [(1, 5), (3, 40), (70, 33)])
+def test_int8_linear_without_inner_dimension(B, M, N):
+    import torch
+    bias = torch.randn(N, device="cuda")
+    got = B.adapt_int8_linear(torch.empty((M, 0), dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda"), torch.empty((N, 0), dtype=torch.int8, device="cuda"),
+                              torch.ones(N, device="cuda"), bias=bias)
+    assert torch.equal(got, bias.expand(M, N))
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 512, 64), (20, 256, 128), (130, 384, 130), (260, 512, 260)])
+def test_int8_linear_at_odd_addresses(B, M, K, N):
+    """Operands at any byte, results at an element's own alignment; nothing is written beside the result."""
+    import torch
+    rng = np.random.default_rng(M)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    for ao, wo in ((3, 0), (0, 5), (1, 2)):
+        fa, fw = torch.empty(M * K + 8, dtype=torch.int8, device="cuda"), torch.empty(N * K + 8, dtype=torch.int8, device="cuda")
+        fa[ao:ao + M * K] = dev(a).view(-1)
+        fw[wo:wo + N * K] = dev(w).view(-1)
+        out = torch.full((M * N + 2,), 77.0, dtype=torch.bfloat16, device="cuda")
+        B.adapt_int8_linear(fa[ao:ao + M * K].view(M, K), dev(s_a), fw[wo:wo + N * K].view(N, K), dev(s_w), out=out[1:-1].view(M, N))
+        same_bits(out[1:-1].view(M, N), rounded(ot.int8_linear(a, s_a, w, s_w), "bf16"))
+        assert out[0] == 77 and out[-1] == 77
+
+
+def test_int8_linear_has_the_integers_of_the_exact_table(B):
+    from paper_2203_04071_amd import workloads as wl
+    rng = np.random.default_rng(12)
+    M, K, N = 150, 333, 70
+    a, w = codes(rng, M, K), codes(rng, N, K)
+    acc = B.adapt_approx_linear(B.Lut(wl.exact_lut(8), 8), dev(a), dev(w))
+    got = B.adapt_int8_linear(dev(a), dev(np.ones(M, np.float32)), dev(w), dev(np.ones(N, np.float32)))
+    assert (got == acc.float()).all()
+
+
+# ---------------------------------------------------------------------------------------------- gradients of the product
+
+GRADIENTS = [(1, 1, 1), (1, 512, 64), (3, 5, 7), (64, 48, 32), (65, 33, 31), (100, 128, 130), (128, 256, 64), (130, 260, 270), (257, 64, 513), (500, 300, 8),
+             (8, 300, 500), (640, 512, 256), (31, 1000, 17), (2, 16, 1025)]
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", GRADIENTS)
+def test_int8_linear_backward(B, name, M, K, N):
+    rng = np.random.default_rng(M + 17 * K + 31 * N)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    dy, dyd = randn(rng, (M, N), name)
+    dx, dw, db = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w))
+    (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+    kept = 0.0 if name == "f32" else 2.0 ** -17
+    within(dx, wx, mx, N, name, kept)
+    within(dw, ww, mw, M, name, kept)
+    within(db, wb, mb, M, name)
+    # the same call again: the same bits; each gradient alone: the same bits
+    dx2, dw2, db2 = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w), want=("dx",)) [0], \
+        B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w), want=("dw",))[1], \
+        B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w), want=("db",))[2]
+    same_bits(dx2, dx.cpu())
+    same_bits(dw2, dw.cpu())
+    same_bits(db2, db.cpu())
+
+
+@pytest.mark.parametrize("exponent", [-140, -126, -118, -100, 90])
+def test_int8_linear_backward_over_the_range_of_fp32(B, exponent):
+    """Small and large gradients keep their bits (the products with the codes stay in range)."""
+    rng = np.random.default_rng(exponent + 500)
+    M, K, N = 96, 80, 70
+    a, w = codes(rng, M, K), codes(rng, N, K)
+    s_a, s_w = np.exp2(rng.integers(-1, 2, M)).astype(np.float32), np.exp2(rng.integers(-1, 2, N)).astype(np.float32)
+    dy = np.ldexp(rng.standard_normal((M, N)), exponent).astype(np.float32)
+    dx, dw, db = B.adapt_int8_linear_backward(dev(dy), dev(a), dev(s_a), dev(w), dev(s_w))
+    # forming dy * s may round a subnormal: half of 2^-149 for each term, times a code of up to 128
+    (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+    within(dx, wx, mx + N * 128 * 2.0 ** -125, N, "f32")
+    within(dw, ww, mw + M * 128 * 2.0 ** -125, M, "f32")
+    within(db, wb, mb, M, "f32")
+
+
+def test_int8_linear_backward_infinities_and_nan_stay_in_their_rows(B):
+    import torch
+    rng = np.random.default_rng(9)
+    M, K, N = 70, 90, 66
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    w[:, 0], a[:, 0] = 1, 1
+    dy = rng.standard_normal((M, N)).astype(np.float32)
+    dy[5, 7], dy[9, 11] = np.inf, np.nan
+    dx, dw, db = (t.cpu() for t in B.adapt_int8_linear_backward(dev(dy), dev(a), dev(s_a), dev(w), dev(s_w)))
+    assert dx[5, 0] == np.inf and torch.isnan(dx[9]).all() and dw[7, 0] == np.inf and torch.isnan(dw[11]).all()
+    assert db[7] == np.inf and torch.isnan(db[11])
+    rows, cols = [i for i in range(M) if i not in (5, 9)], [i for i in range(N) if i not in (7, 11)]
+    assert torch.isfinite(dx[rows]).all() and torch.isfinite(dw[cols]).all() and torch.isfinite(db[cols]).all()
+
+
+def test_int8_linear_backward_empty(B):
+    import torch
+
+    def call(M, K, N):
+        z = lambda *s: torch.zeros(s, dtype=torch.int8, device="cuda")
+        return B.adapt_int8_linear_backward(torch.ones((M, N), device="cuda"), z(M, K), torch.ones(M, device="cuda"), z(N, K), torch.ones(N, device="cuda"))
+    dx, dw, db = call(0, 8, 9)
+    assert dx.shape == (0, 8) and (dw == 0).all() and (db == 0).all()
+    dx, dw, db = call(7, 8, 0)
+    assert (dx == 0).all() and dx.shape == (7, 8) and dw.shape == (0, 8) and db.shape == (0,)
+    dx, dw, db = call(7, 0, 5)
+    assert dx.shape == (7, 0) and dw.shape == (5, 0) and (db == 7).all()
+
+
+def test_int8_linear_backward_against_differences(B):
+    """The layer is linear in each scale: moving a token's scale moves sum(dy * y) by sum_k dx[m][k] a[m][k]; likewise a channel's."""
+    rng = np.random.default_rng(21)
+    M, K, N = 40, 64, 48
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    dy = rng.standard_normal((M, N)).astype(np.float32)
+    dx, dw, _ = B.adapt_int8_linear_backward(dev(dy), dev(a), dev(s_a), dev(w), dev(s_w))
+
+    def loss(sa, sw):
+        return (dy.astype(np.float64) * f64(B.adapt_int8_linear(dev(a), dev(sa), dev(w), dev(sw)))).sum()
+    base = loss(s_a, s_w)
+    for m in (0, 17, 39):
+        s2 = s_a.copy()
+        s2[m] *= 2          # exact in fp32: the difference is the row's own term
+        want = (f64(dx)[m] * a[m]).sum() * float(s_a[m])
+        assert abs(loss(s2, s_w) - base - want) <= 1e-5 * np.abs(f64(dx)[m] * a[m]).sum() * s_a[m] + 1e-5 * N
+    for n in (0, 20, 47):
+        s2 = s_w.copy()
+        s2[n] *= 2
+        want = (f64(dw)[n] * w[n]).sum() * float(s_w[n])
+        assert abs(loss(s_a, s2) - base - want) <= 1e-5 * np.abs(f64(dw)[n] * w[n]).sum() * s_w[n] + 1e-5 * M
+
+
+# ---------------------------------------------------------------------------------------------- embedding
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("T,V,D", [(1, 1, 1), (5, 3, 4), (100, 50, 512), (33, 7, 33), (9, 1000, 1027), (3, 20, 5000), (4097, 300, 24), (64, 100, 128)])
+def test_embedding(B, name, T, V, D):
+    rng = np.random.default_rng(T + V + D)
+    table, td = randn(rng, (V, D), name)
+    for dtype in (np.int64, np.int32):
+        tok = rng.integers(-2, V + 2, T).astype(dtype)          # some outside the table
+        same_bits(B.adapt_embedding(td, dev(tok), scale=1.7), rounded(ot.embedding(table, tok, 1.7), name))
+    tok[:] = V - 1
+    same_bits(B.adapt_embedding(td, dev(tok.reshape(1, T))), rounded(ot.embedding(table, tok, 1.0)[None], name))
+
+
+def test_embedding_tokens_far_outside(B):
+    tok = np.array([0, -1, 2 ** 31, 2 ** 32, 2 ** 40 + 1, -2 ** 63, 2 ** 63 - 1, 2], np.int64)
+    table = np.arange(1, 13, dtype=np.float32).reshape(3, 4)
+    same_bits(B.adapt_embedding(dev(table), dev(tok)), rounded(ot.embedding(table, tok, 1.0), "f32"))
+    dy = np.ones((8, 4), np.float32)
+    assert (f64(B.adapt_embedding_backward(dev(dy), dev(tok), 3)) == ot.embedding_backward(dy, tok, 3, 1.0)[0]).all()
+
+
+def test_embedding_empty_table(B):
+    import torch
+    y = B.adapt_embedding(torch.empty((0, 6), device="cuda"), dev(np.zeros(4, np.int64)))
+    assert (y == 0).all() and y.shape == (4, 6)
+    assert B.adapt_embedding_backward(y, dev(np.zeros(4, np.int64)), 0).shape == (0, 6)
+
+
+def tokens_of(rng, kind, T, V):
+    if kind == "uniform":
+        return rng.integers(0, V, T)
+    if kind == "zipf":
+        return np.minimum(np.exp(rng.uniform(0, np.log(V + 1), T)).astype(np.int64) - 1, V - 1)
+    if kind == "one":
+        return np.full(T, V // 2)
+    if kind == "outside":
+        return rng.integers(-V, 2 * V, T)
+    if kind == "none":
+        return np.full(T, -1)
+    return np.sort(rng.integers(0, V, T))[::-1].copy()         # "sorted", downwards
+
+
+@pytest.mark.parametrize("kind", ["uniform", "zipf", "one", "outside", "none", "sorted"])
+@pytest.mark.parametrize("T,V,D", [(1, 1, 1), (31, 5, 16), (64, 600, 33), (2049, 40, 8), (5000, 3000, 65), (1500, 1 << 19, 4), (700, 20, 1030)])
+def test_embedding_backward(B, kind, T, V, D):
+    rng = np.random.default_rng(T + V + D)
+    for name, dtype, pad in (("f32", np.int64, -1), ("bf16", np.int32, 0), ("f16", np.int64, V // 2)):
+        tok = tokens_of(rng, kind, T, V).astype(dtype)
+        dy, dyd = randn(rng, (T, D), name)
+        got = B.adapt_embedding_backward(dyd, dev(tok), V, scale=1.5, padding_idx=pad)
+        want, mass, n = ot.embedding_backward(dy, tok, V, 1.5, pad)
+        within(got, want, mass, n[:, None], name)
+        assert (f64(got)[n == 0] == 0).all()
+
+
+@pytest.mark.parametrize("T,V,D", [(40000, 50000, 64), (70001, 12, 40), (20000, 70000, 16)])
+def test_embedding_backward_long_runs(B, T, V, D):
+    """Runs of thousands of places; the sum does not depend on the order in which the places come (permuted with their
+    gradients, a token's places keep their order, so its bits stay)."""
+    rng = np.random.default_rng(T)
+    tok = tokens_of(rng, "zipf", T, V)
+    tok[rng.random(T) < 0.4] = 3
+    dy, dyd = randn(rng, (T, D), "f32")
+    got = B.adapt_embedding_backward(dyd, dev(tok), V)
+    want, mass, n = ot.embedding_backward(dy, tok, V, 1.0)
+    within(got, want, mass, n[:, None], "f32")
+    same_bits(B.adapt_embedding_backward(dyd, dev(tok), V), got.cpu())
+
+
+def test_embedding_backward_in_a_used_workspace(B):
+    """Whatever the workspace holds from other calls does not matter, and a larger one serves."""
+    import torch
+    rng = np.random.default_rng(2)
+    ws = torch.full((1 << 24,), 0xFF, dtype=torch.uint8, device="cuda")
+    for T, V, D in ((3000, 777, 24), (17, 4000, 24), (900, 3, 100)):
+        tok = tokens_of(rng, "zipf", T, V)
+        dy, dyd = randn(rng, (T, D), "f32")
+        got = B.adapt_embedding_backward(dyd, dev(tok), V, workspace=ws)
+        want, mass, n = ot.embedding_backward(dy, tok, V, 1.0)
+        within(got, want, mass, n[:, None], "f32")
+
+
+# ---------------------------------------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("n", [1, 3, 4, 5, 7, 8, 9, 255, 1023, 4097, 100003, 1 << 20])
+def test_dropout(B, name, n):
+    import torch
+    rng = np.random.default_rng(n)
+    x, xd = randn(rng, (n,), name)
+    for p, seed, offset in ((0.5, 0, 0), (0.1, 0x123456789ABCDEF, 3), (1e-9, 2, 1 << 40), (0.999, (1 << 64) - 1, (1 << 64) - 1)):
+        want = rounded(ot.dropout(x, p, seed, offset), name)
+        same_bits(B.adapt_dropout(xd, p, seed, offset), want)
+        same_bits(B.adapt_dropout_backward(xd, p, seed, offset), want)
+    same_bits(B.adapt_dropout(xd, 0.0, 5), xd.cpu())
+    assert (B.adapt_dropout(xd, 1.0, 5) == 0).all()
+    # in place, from the middle of a buffer, on a step of the device's
+    flat = torch.full((n + 2,), 9.0, dtype=_t(name), device="cuda")
+    flat[1:-1] = xd
+    step = torch.tensor([7], dtype=torch.int64, device="cuda")
+    B.adapt_dropout(flat[1:-1], 0.25, 99, 1000, step=step, out=flat[1:-1])
+    same_bits(flat[1:-1], rounded(ot.dropout(x, 0.25, 99, 1007), name))
+    assert flat[0] == 9 and flat[-1] == 9
+
+
+def test_dropout_drops_infinities_and_nan(B):
+    x = np.where(np.arange(4096) % 2 == 0, np.inf, np.nan).astype(np.float32)
+    kept = ot.dropout_kept(4096, 0.5, 3, 0)
+    got = f64(B.adapt_dropout(dev(x), 0.5, 3))
+    assert (got[~kept] == 0).all() and np.isinf(got[kept & (np.arange(4096) % 2 == 0)]).all() and np.isnan(got[kept & (np.arange(4096) % 2 == 1)]).all()
+    assert (f64(B.adapt_dropout(dev(x), 1.0, 3)) == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------- together
+
+def _step(B, c, ws=None):
+    """tokens -> embedding -> dropout -> codes -> product, and back to the gradients of the table and of the weights"""
+    e = B.adapt_embedding(c["table"], c["tok"], scale=2.0)
+    x = B.adapt_dropout(e, 0.2, 77, 4, step=c["step"])
+    a, s_a = B.adapt_quantize_tokens(x, 8)
+    y = B.adapt_int8_linear(a, s_a, c["w"], c["s_w"], bias=c["bias"], dtype=c["table"].dtype)
+    dx, dw, db = B.adapt_int8_linear_backward(c["dy"], a, s_a, c["w"], c["s_w"])
+    de = B.adapt_dropout_backward(dx, 0.2, 77, 4, step=c["step"])
+    dt = B.adapt_embedding_backward(de, c["tok"], c["table"].shape[0], scale=2.0, padding_idx=0)
+    return dict(y=y, dw=dw, db=db, dt=dt, a=a, s_a=s_a, x=x, de=de)
+
+
+def _inputs(name, T, V, D, N, seed=1):
+    import torch
+    rng = np.random.default_rng(seed)
+    table, td = randn(rng, (V, D), name)
+    tok = tokens_of(rng, "zipf", T, V)
+    w, s_w = codes(rng, N, D), scales(rng, N)
+    bias = rng.standard_normal(N).astype(np.float32)
+    dy, dyd = randn(rng, (T, N), name)
+    return dict(table=td, tok=dev(tok), w=dev(w), s_w=dev(s_w), bias=dev(bias), dy=dyd, step=torch.zeros(1, dtype=torch.int64, device="cuda")), \
+        dict(table=table, tok=tok, w=w, s_w=s_w, bias=bias, dy=dy)
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("T,V,D,N", [(100, 50, 64, 48), (333, 1000, 129, 77)])
+def test_a_training_step_of_the_text_path(B, name, T, V, D, N):
+    c, h = _inputs(name, T, V, D, N)
+    got = _step(B, c)
+    e = rounded(ot.embedding(h["table"], h["tok"], 2.0), name)
+    x = rounded(ot.dropout(e.float().numpy(), 0.2, 77, 4), name)
+    same_bits(got["x"], x)
+    a, s_a = ot.quantize_tokens(x.float().numpy(), 8)
+    assert (got["a"].cpu().numpy() == a).all() and (got["s_a"].cpu().numpy() == s_a).all()
+    same_bits(got["y"], rounded(ot.int8_linear(a, s_a, h["w"], h["s_w"], h["bias"]), name))
+    (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(h["dy"], a, s_a, h["w"], h["s_w"])
+    kept = 0.0 if name == "f32" else 2.0 ** -17
+    within(got["dw"], ww, mw, T, name, kept)
+    within(got["db"], wb, mb, T, name)
+    want, mass, n = ot.embedding_backward(got["de"].float().cpu().numpy(), h["tok"], V, 2.0, 0)
+    within(got["dt"], want, mass, n[:, None], name)
+
+
+def test_a_captured_step_draws_a_new_mask_at_every_replay(B):
+    """The whole step recorded once: replays equal the eager step on the same device counter, with eager work between them."""
+    import torch
+    c, _ = _inputs("bf16", 700, 300, 128, 96)
+    _step(B, c)                                     # (the first calls of a process load the kernels)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rec = _step(B, c)
+    seen = []
+    for step in (0, 1, 5):
+        c["step"].fill_(step)
+        torch.cuda.synchronize()
+        want = _step(B, c)
+        torch.cuda.synchronize()
+        for _ in range(2):
+            g.replay()
+            torch.cuda.synchronize()
+            for k in rec:
+                assert torch.equal(rec[k], want[k]), (step, k)
+        seen.append(want["x"].clone())
+    assert not torch.equal(seen[0], seen[1]) and not torch.equal(seen[1], seen[2])
+
+
+def test_calls_on_two_streams_at_once(B):
+    """Calls share nothing: two streams, each with its own operands, results as on one."""
+    import torch
+    cs = [_inputs("f32", 900, 200, 96, 80, seed=s)[0] for s in (1, 2)]
+    want = [_step(B, c) for c in cs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [None, None]
+    for _ in range(3):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i] = _step(B, cs[i])
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            for k in want[i]:
+                assert torch.equal(got[i][k], want[i][k]), (i, k)
+
+
+def test_a_stream_given_to_the_call(B):
+    """With `stream`, results and workspaces are that stream's memory."""
+    import torch
+    rng = np.random.default_rng(6)
+    s = torch.cuda.Stream()
+    tok = tokens_of(rng, "zipf", 5000, 300)
+    dy, dyd = randn(rng, (5000, 64), "f32")
+    td = dev(tok)
+    want = B.adapt_embedding_backward(dyd, td, 300)
+    torch.cuda.synchronize()
+    got = [B.adapt_embedding_backward(dyd, td, 300, stream=s) for _ in range(4)]
+    noise = [torch.full((1 << 22,), 3.0, device="cuda") for _ in range(4)]
+    s.synchronize()
+    assert all(torch.equal(g, want) for g in got) and noise[0][0] == 3.0
+
+
+def test_binding_refuses_what_it_cannot_pass_on(B):
+    import torch
+    a = torch.zeros((4, 8), dtype=torch.int8, device="cuda")
+    s = torch.ones(4, device="cuda")
+    with pytest.raises(ValueError):
+        B.adapt_int8_linear(a, s[:3].contiguous(), a, s)
+    with pytest.raises(ValueError):
+        B.adapt_int8_linear(a, s, torch.zeros((4, 9), dtype=torch.int8, device="cuda"), s)
+    with pytest.raises(TypeError):
+        B.adapt_int8_linear(a.t(), torch.ones(8, device="cuda"), a.t(), torch.ones(8, device="cuda"))
+    with pytest.raises(TypeError):
+        B.adapt_quantize_tokens(torch.zeros((2, 2), dtype=torch.float64, device="cuda"))
+    with pytest.raises(TypeError):
+        B.adapt_embedding(torch.zeros((2, 2), device="cuda"), torch.zeros(3, device="cuda"))
+    with pytest.raises(TypeError):
+        B.adapt_dropout(torch.zeros(4), 0.5, 1)
+    with pytest.raises(B.AdaptError) as e:
+        B.adapt_dropout(torch.zeros(4, device="cuda"), 1.5, 1)
+    assert e.value.code == -1
