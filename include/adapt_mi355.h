@@ -552,9 +552,9 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
  *     db[n]    = sum_m dy[m][n]
  * dy_dev [M][N], dx_dev [M][K], dw_dev [N][K], db_dev [N] of element type `type`; codes and scales as in adapt_int8_linear.  Any of dx_dev,
  * dw_dev, db_dev may be NULL (not computed; a_dev and s_a_dev are read for dw alone, w_dev and s_w_dev for dx alone).  They are
- * fully overwritten.  dy * s is formed in fp32 and kept to 24 bits (ADAPT_F32) or 16 bits (the 16-bit types, whose results keep 8 or 11).
+ * fully overwritten.  M, K and N are at most 65535 * 64, M and N at most 2796160 (ADAPT_F32) (else ADAPT_ERR_UNSUPPORTED).  dy * s is formed in fp32 and kept to 24 bits (ADAPT_F32) or 16 bits (the 16-bit types, whose results keep 8 or 11).
  * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
- * dx_dev / dw_dev are given).  2^34 gradients or more in one matrix: ADAPT_ERR_UNSUPPORTED. */
+ * dx_dev / dw_dev are given). */
 int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes);
 int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev,
                                int M, int K, int N, void *dx_dev, void *dw_dev, void *db_dev, void *workspace_dev, size_t workspace_bytes,

@@ -880,12 +880,10 @@ def _new(stream, shape, dtype):
 
 
 def _workspace(workspace, need, stream):
-    """The caller's uint8 tensor if it is large enough, else a new one that lives until the call's kernels have run."""
-    if need == 0:
-        return None, 0
+    """The caller's uint8 tensor if it is large enough, else a new one, which the calling function holds until its kernels are enqueued."""
     if workspace is None or workspace.numel() < need:
         workspace = _new(stream, (need,), torch.uint8)
-    return ctypes.c_void_p(_ptr(workspace, torch.uint8)), workspace.numel()
+    return workspace
 
 
 def adapt_quantize_tokens(x, bits: int = 8, out=None, scales=None, stream=None):
@@ -933,12 +931,12 @@ def adapt_int8_linear_backward(dy, a, s_a, w, s_w, want=("dx", "dw", "db"), work
     _here(dy, a, s_a, w, s_w, workspace)
     need = ctypes.c_size_t(0)
     _chk(load().adapt_int8_linear_backward_workspace(M, K, N, _element(dy), int("dx" in want), int("dw" in want), ctypes.byref(need)))
-    ws, ws_bytes = _workspace(workspace, need.value, stream)
+    ws = _workspace(workspace, need.value, stream)
     dx = _new(stream, (M, K), dy.dtype) if "dx" in want else None
     dw = _new(stream, (N, K), dy.dtype) if "dw" in want else None
     db = _new(stream, (N,), dy.dtype) if "db" in want else None
     _chk(load().adapt_int8_linear_backward(_ptr(dy), _element(dy), _ptr(a, torch.int8), _ptr(s_a, torch.float32), _ptr(w, torch.int8),
-                                           _ptr(s_w, torch.float32), M, K, N, _ptr(dx), _ptr(dw), _ptr(db), ws, ws_bytes, _stream(stream)))
+                                           _ptr(s_w, torch.float32), M, K, N, _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws, torch.uint8), ws.numel(), _stream(stream)))
     return dx, dw, db
 
 
@@ -971,10 +969,10 @@ def adapt_embedding_backward(dy, tokens, V: int, scale: float = 1.0, padding_idx
     _shape("out", out, (V, D))
     need = ctypes.c_size_t(0)
     _chk(load().adapt_embedding_backward_workspace(tokens.numel(), V, D, ctypes.byref(need)))
-    ws, ws_bytes = _workspace(workspace, need.value, stream)
+    ws = _workspace(workspace, need.value, stream)
     tok, tok_bits = _tokens(tokens)
-    _chk(load().adapt_embedding_backward(_ptr(dy), _element(dy), tok, tok_bits, _ptr(out, dy.dtype), tokens.numel(), V, D, float(scale), padding_idx, ws,
-                                         ws_bytes, _stream(stream)))
+    _chk(load().adapt_embedding_backward(_ptr(dy), _element(dy), tok, tok_bits, _ptr(out, dy.dtype), tokens.numel(), V, D, float(scale), padding_idx,
+                                         _ptr(ws, torch.uint8), ws.numel(), _stream(stream)))
     return out
 
 

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadapt_mi355.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("api_core.hip", "api_layers.hip", "byte_kernels.hip", "api_i16.hip", "api_backward.hip", "api_tokens.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("api_core.hip", "api_layers.hip", "byte_kernels.hip", "api_i16.hip", "api_backward.hip", "api_int8.hip", "api_tokens.hip")]
 # ceiling probes for bench.py: a library of their own, not part of the product
 PROBES_LIB = os.path.join(HERE, "libadapt_probes.so")
 PROBES_SOURCE = os.path.join(CSRC, "probes.hip")

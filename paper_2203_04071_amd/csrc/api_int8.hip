@@ -1,0 +1,271 @@
+// C ABI, part 5: the exact 8-bit product with a scale for each token and channel, and its gradients.
+#include "api_common.hpp"
+#include "int8_gradient.hpp"
+#include "int8_linear.hpp"
+#include "tile_plan.hpp"
+
+using namespace adapt_api;
+
+namespace {
+
+bool off_by(const void *p, size_t align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int INT8_MAX_K = 131071;              // (-128)^2 K < 2^31
+constexpr long long MAX_TILES = 1ll << 24;      // a launch is limited to 2^32 threads
+constexpr int GRAD_MAX = 65535 * 64;            // a grid's second dimension
+
+int int8_args(const char *who, int M, int K, int N, int type) {
+    if (M < 0 || K < 0 || N < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
+    if (!adapt::element_size(type)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
+    return ADAPT_OK;
+}
+
+template <class Op, class E, int TM, int TN, int SB, int NB, bool DMA, bool TANH = false>
+void launch_tile(adapt::TileParams p, const TilePlan &t, hipStream_t s) {
+    p.tiles_i = (int)t.tiles_i;
+    p.tiles_j = (int)t.tiles_j;
+    p.Kb_split = (int)t.kb_split;
+    adapt::tile_product_kernel<Op, E, TM, TN, SB, NB, DMA, TANH><<<dim3((unsigned)(t.tiles_i * t.tiles_j), (unsigned)t.split), adapt::TILE_THREADS, 0, s>>>(p);
+}
+
+// whole stages go from memory to LDS by themselves: rows of 16-byte pieces
+template <class Op, class E>
+void launch_tiles(const adapt::TileParams &p, const TilePlan &t, hipStream_t s) {
+    switch (t.kind) {
+        case TILE_256x256: launch_tile<Op, E, 256, 256, 64, 4, true>(p, t, s); break;
+        case TILE_256x128: launch_tile<Op, E, 256, 128, 128, 3, true>(p, t, s); break;
+        case TILE_128x128: launch_tile<Op, E, 128, 128, 128, 4, true>(p, t, s); break;
+        case TILE_128x64: launch_tile<Op, E, 128, 64, 128, 4, true>(p, t, s); break;
+        default: launch_tile<Op, E, 64, 64, 128, 4, true>(p, t, s); break;
+    }
+}
+
+TilePlan one_tile(long long I, long long J, long long Kb, int tm, int tn) {
+    return TilePlan{TILE_KINDS, tm, tn, (I + tm - 1) / tm, (J + tn - 1) / tn, 1, Kb};
+}
+
+template <class E, int MT, bool TANH = false>
+void launch_tokens(const adapt::Int8Params &p, hipStream_t s) {
+    const dim3 grid((unsigned)(((long long)p.N + 15) / 16), (unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
+    adapt::int8_tokens_kernel<E, MT, 8, TANH><<<grid, 512, 0, s>>>(p);
+}
+
+// Few tokens, or few tiles: the kernel without LDS tiles (int8_tokens_kernel) reads 16 (MT + 1) K bytes per workgroup of 16 x 16 MT outputs, at about
+// 13 TB/s from L2; a tile of 64 x 64 takes K / 128 stages of 0.15 us whatever the number of tiles, up to two per compute unit.  They meet where
+// (MT + 1) times the number of workgroups is 900: 32 x 4096 x 4096 8.1 us against 10.4, 64 x 4096 x 4096 11.6 against 10.1, 64 x 8192 -> 256
+// 9.1 against 17, 8 x 4096 -> 16384 17 against 12.6.  Rows that are no multiple of 16 bytes (up to 64 tokens): always.
+int tokens_kernel_mt(int M, int N, bool dma) {
+    const long long n16 = ((long long)N + 15) / 16;
+    const int mts[3] = {1, 2, 4};
+    int best = 0;
+    long long best_cost = 0;
+    for (int mt : mts) {
+        const long long cost = (mt + 1) * n16 * ((M + 16 * mt - 1) / (16 * mt));
+        if (!best || cost < best_cost) {
+            best = mt;
+            best_cost = cost;
+        }
+    }
+    // (few workgroups: smaller ones, to have more)
+    for (int mt : mts) {
+        const long long groups = n16 * ((M + 16 * mt - 1) / (16 * mt));
+        if (mt < best && (mt + 1) * groups < 450) {
+            best = mt;
+            best_cost = (mt + 1) * groups;
+            break;
+        }
+    }
+    return best_cost < 900 || (!dma && M <= 64) ? best : 0;
+}
+
+template <class E>
+void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
+    const bool dma = q.K % 16 == 0 && aligned16(q.a) && aligned16(q.w);
+    adapt::TileParams p{};
+    p.a = reinterpret_cast<const char *>(q.a);
+    p.b = reinterpret_cast<const char *>(q.w);
+    p.I = q.M;
+    p.J = q.N;
+    p.Kb = q.K;
+    p.lda = p.ldb = (uint32_t)q.K;
+    p.s_i = q.s_a;
+    p.s_j = q.s_w;
+    p.bias = q.bias;
+    p.act = q.act;
+    p.c = q.y;
+    const TilePlan small = one_tile(p.I, p.J, p.Kb, 64, 64);
+    if (q.act == 2) {       // (tanh: one kernel for each way of reading)
+        if (q.M <= 16) launch_tokens<E, 1, true>(q, s);
+        else if (dma) launch_tile<adapt::TileI8, E, 64, 64, 128, 4, true, true>(p, small, s);
+        else launch_tile<adapt::TileI8, E, 64, 64, 256, 2, false, true>(p, small, s);
+        return;
+    }
+    switch (tokens_kernel_mt(q.M, q.N, dma)) {
+        case 1: launch_tokens<E, 1>(q, s); return;
+        case 2: launch_tokens<E, 2>(q, s); return;
+        case 4: launch_tokens<E, 4>(q, s); return;
+    }
+    if (dma) launch_tiles<adapt::TileI8, E>(p, tile_plan(p.I, p.J, p.Kb, device_cus(), 1), s);
+    else launch_tile<adapt::TileI8, E, 64, 64, 256, 2, false>(p, small, s);
+}
+
+// Workspace of one gradient c [I][J], the sums over R: rows of the pieces of dy s [I], rows of codes [J], partial sums of a split
+// product.
+struct GradPlan {
+    int Rp;                     // R in whole stages
+    long long row;              // bytes of a row: all pieces
+    TilePlan tile;
+    size_t b, part, bytes;      // offsets (a at 0)
+};
+GradPlan grad_plan(long long I, long long J, long long R, int P) {
+    GradPlan g{};
+    g.Rp = (int)((R + adapt::GRAD_STAGE - 1) / adapt::GRAD_STAGE * adapt::GRAD_STAGE);
+    g.row = 2ll * P * g.Rp;
+    g.tile = tile_plan(I, J, g.row, device_cus(), 8);
+    g.b = round256((size_t)I * (size_t)g.row);
+    g.part = g.b + round256((size_t)J * (size_t)g.row);
+    g.bytes = g.part + (g.tile.split > 1 ? round256((size_t)g.tile.split * (size_t)I * (size_t)J * 4) : 0);
+    return g;
+}
+int grad_pieces(int type) { return type == ADAPT_F32 ? 3 : 2; }
+
+size_t db_blocks(int M) { return ((size_t)M + adapt::GRAD_DB_ROWS - 1) / adapt::GRAD_DB_ROWS; }
+
+template <class E>
+void join(const float *part, int parts, size_t n, void *c, hipStream_t s) {
+    adapt::grad_join_kernel<E><<<ew_grid(n / 4 + 1), 256, 0, s>>>(part, parts, n, static_cast<typename E::mem *>(c));
+}
+
+template <class E>
+void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_t s) {
+    adapt::TileParams p{};
+    p.a = ws;
+    p.b = ws + g.b;
+    p.I = I;
+    p.J = J;
+    p.Kb = (int)g.row;
+    p.lda = p.ldb = (uint32_t)g.row;
+    if (g.tile.split == 1) {
+        p.c = c;
+        launch_tiles<adapt::TileBF16, E>(p, g.tile, s);
+    } else {
+        p.c = ws + g.part;
+        launch_tiles<adapt::TileBF16, adapt::F32>(p, g.tile, s);
+        join<E>(reinterpret_cast<const float *>(ws + g.part), g.tile.split, (size_t)I * (size_t)J, c, s);
+    }
+}
+
+dim3 blocks64(int R, int C) { return dim3((unsigned)((R + 63) / 64), (unsigned)((C + 63) / 64)); }
+
+template <class E, int P>
+void gradients(const adapt::Int8Params &q, const void *dy_dev, void *dx, void *dw, void *db, char *ws, hipStream_t s) {
+    const typename E::mem *const dy = static_cast<const typename E::mem *>(dy_dev);
+    __bf16 *const a = reinterpret_cast<__bf16 *>(ws);
+    if (dx) {
+        const GradPlan g = grad_plan(q.M, q.K, q.N, P);
+        __bf16 *const b = reinterpret_cast<__bf16 *>(ws + g.b);
+        if (g.Rp) {
+            adapt::grad_split_rows_kernel<E, P><<<ew_grid((size_t)q.M * g.Rp / 8), 256, 0, s>>>(dy, q.s_w, a, q.M, q.N, g.Rp);
+            adapt::grad_codes_kernel<P><<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.w, b, q.N, q.K, g.Rp);
+        }
+        grad_product<E>(g, ws, q.M, q.K, dx, s);
+    }
+    if (dw) {
+        const GradPlan g = grad_plan(q.N, q.K, q.M, P);
+        __bf16 *const b = reinterpret_cast<__bf16 *>(ws + g.b);
+        if (g.Rp) {
+            adapt::grad_split_columns_kernel<E, P><<<blocks64(g.Rp, q.N), 256, 0, s>>>(dy, q.s_a, a, q.M, q.N, g.Rp);
+            adapt::grad_codes_kernel<P><<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.a, b, q.M, q.K, g.Rp);
+        }
+        grad_product<E>(g, ws, q.N, q.K, dw, s);
+    }
+    if (db) {
+        float *const part = reinterpret_cast<float *>(ws);
+        const size_t blocks = db_blocks(q.M);
+        if (blocks) adapt::grad_bias_kernel<E><<<dim3((unsigned)blocks, (unsigned)((q.N + 63) / 64)), 256, 0, s>>>(dy, part, q.M, q.N);
+        else adapt::fill_u32_kernel<<<ew_grid((size_t)q.N), 256, 0, s>>>(reinterpret_cast<uint32_t *>(part), 0u, (size_t)q.N);
+        join<E>(part, blocks ? (int)blocks : 1, (size_t)q.N, db, s);
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev, const float *bias_dev, int act,
+                      void *y_dev, int y_type, int M, int K, int N, void *stream) {
+    const char *who = "adapt_int8_linear";
+    if (int rc = int8_args(who, M, K, N, y_type)) return rc;
+    if (act < 0 || act > 2) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: act=%d not in [0,2]", who, act);
+    if (!M || !N) return ADAPT_OK;
+    if (!s_a_dev || !s_w_dev || !y_dev || (K && (!a_dev || !w_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
+    if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4) || off_by(bias_dev, 4) || off_by(y_dev, (size_t)adapt::element_size(y_type)))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    for (const void *q : {(const void *)a_dev, (const void *)w_dev, (const void *)s_a_dev, (const void *)s_w_dev, (const void *)bias_dev})
+        if (q == y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
+    if (K > INT8_MAX_K) return fail(ADAPT_ERR_UNSUPPORTED, "%s: K=%d above %d, sums could pass 32 bits", who, K, INT8_MAX_K);
+    if ((((long long)M + 63) / 64) * (((long long)N + 63) / 64) >= MAX_TILES) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^36 outputs or more", who);
+    const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, bias_dev, y_dev, M, K, N, act};
+    ADAPT_FOR_TYPE(y_type, E, launch_int8<E>(p, (hipStream_t)stream));
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes) {
+    const char *who = "adapt_int8_linear_backward_workspace";
+    if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
+    *bytes = 0;
+    if (int rc = int8_args(who, M, K, N, type)) return rc;
+    if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
+    const int P = grad_pieces(type);
+    // (the bias gradient's partial sums are at home in any of it)
+    size_t need = round256((db_blocks(M) + 1) * (size_t)N * 4);
+    if (want_dx && M && K) {
+        const size_t b = grad_plan(M, K, N, P).bytes;
+        need = b > need ? b : need;
+    }
+    if (want_dw && N && K) {
+        const size_t b = grad_plan(N, K, M, P).bytes;
+        need = b > need ? b : need;
+    }
+    *bytes = need;
+    return ADAPT_OK;
+}
+
+int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev,
+                               int M, int K, int N, void *dx_dev, void *dw_dev, void *db_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
+    const char *who = "adapt_int8_linear_backward";
+    if (int rc = int8_args(who, M, K, N, type)) return rc;
+    const size_t e = (size_t)adapt::element_size(type);
+    const bool want_dx = dx_dev && M > 0 && K > 0, want_dw = dw_dev && N > 0 && K > 0, want_db = db_dev && N > 0;
+    if (!want_dx && !want_dw && !want_db) return ADAPT_OK;
+    if (M > 0 && N > 0 && !dy_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL dy_dev", who);
+    if (want_dx && N > 0 && (!w_dev || !s_w_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL w_dev / s_w_dev", who);
+    if (want_dw && M > 0 && (!a_dev || !s_a_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL a_dev / s_a_dev", who);
+    for (const void *q : {dy_dev, (const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
+        if (off_by(q, e)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    for (const void *g : {(const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
+        if (g && (g == dy_dev || g == (const void *)a_dev || g == (const void *)w_dev))
+            return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
+    size_t need = 0;
+    if (int rc = adapt_int8_linear_backward_workspace(M, K, N, type, want_dx, want_dw, &need)) return rc;
+    if (need && (!workspace_dev || workspace_bytes < need || off_by(workspace_dev, 256)))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, need);
+    const int P = grad_pieces(type);
+    // (a row of pieces is addressed with 32 bits, 256 rows of it with 32 unsigned)
+    if (2ll * P * (((M > N ? M : N) + 63ll) / 64 * 64) * 256 > 0xffffffffll) return fail(ADAPT_ERR_UNSUPPORTED, "%s: M or N too large", who);
+    const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, nullptr, nullptr, M, K, N, 0};
+    char *const ws = static_cast<char *>(workspace_dev);
+    void *const dx = want_dx ? dx_dev : nullptr, *const dw = want_dw ? dw_dev : nullptr, *const db = want_db ? db_dev : nullptr;
+    hipStream_t s = (hipStream_t)stream;
+    if (type == ADAPT_F32) gradients<adapt::F32, 3>(p, dy_dev, dx, dw, db, ws, s);
+    else if (type == ADAPT_F16) gradients<adapt::F16, 2>(p, dy_dev, dx, dw, db, ws, s);
+    else gradients<adapt::BF16, 2>(p, dy_dev, dx, dw, db, ws, s);
+    HIP_TRY(hipGetLastError());
+    return ADAPT_OK;
+}
+
+}  // extern "C"

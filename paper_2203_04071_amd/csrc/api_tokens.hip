@@ -1,10 +1,9 @@
-// C ABI, part 5: the exact 8-bit product with a scale for each token and channel and its gradients, embedding, dropout.
+// C ABI, part 6: the quantiser with a scale for each token, embedding, dropout.
 #include <cmath>
 
 #include "api_common.hpp"
 #include "dropout.hpp"
 #include "embedding.hpp"
-#include "int8_linear.hpp"
 #include "quantize_tokens.hpp"
 
 using namespace adapt_api;
@@ -14,17 +13,6 @@ namespace {
 bool off_by(const void *p, size_t align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-
-// Tiles of a product: a launch is limited to 2^32 threads, 2^24 workgroups of 256.
-constexpr long long INT8_TILES = 1ll << 24;
-
-constexpr int INT8_MAX_K = 131071;      // (-128)^2 K < 2^31
-
-int int8_args(const char *who, int M, int K, int N, int type) {
-    if (M < 0 || K < 0 || N < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
-    if (!adapt::element_size(type)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
-    return ADAPT_OK;
-}
 
 struct EmbedPlan {
     uint32_t T, V, D, C, pieces, blocks;
@@ -132,65 +120,6 @@ int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *s
     const unsigned grid = cap_grid(tokens, 1u << 20);
     ADAPT_FOR_TYPE(x_type, E, adapt::quantize_tokens_kernel<E><<<grid, adapt::QT_THREADS, 0, (hipStream_t)stream>>>(
                                   static_cast<const E::mem *>(x_dev), q_dev, scales_dev, tokens, cols, Q));
-    HIP_TRY(hipGetLastError());
-    return ADAPT_OK;
-}
-
-int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev, const float *bias_dev, int act,
-                      void *y_dev, int y_type, int M, int K, int N, void *stream) {
-    const char *who = "adapt_int8_linear";
-    if (int rc = int8_args(who, M, K, N, y_type)) return rc;
-    if (act < 0 || act > 2) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: act=%d not in [0,2]", who, act);
-    if (!M || !N) return ADAPT_OK;
-    if (!s_a_dev || !s_w_dev || !y_dev || (K && (!a_dev || !w_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
-    if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4) || off_by(bias_dev, 4) || off_by(y_dev, (size_t)adapt::element_size(y_type)))
-        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    if (K > INT8_MAX_K) return fail(ADAPT_ERR_UNSUPPORTED, "%s: K=%d above %d, sums could pass 32 bits", who, K, INT8_MAX_K);
-    const long long tiles = (((long long)M + 63) / 64) * (((long long)N + 63) / 64);
-    if (tiles >= INT8_TILES) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^36 outputs or more", who);
-    const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, bias_dev, y_dev, M, K, N, act};
-    ADAPT_FOR_TYPE(y_type, E, adapt::int8_linear_kernel<E><<<(unsigned)tiles, 256, 0, (hipStream_t)stream>>>(p));
-    HIP_TRY(hipGetLastError());
-    return ADAPT_OK;
-}
-
-int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes) {
-    const char *who = "adapt_int8_linear_backward_workspace";
-    if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
-    *bytes = 0;
-    if (int rc = int8_args(who, M, K, N, type)) return rc;
-    return ADAPT_OK;
-}
-
-int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev,
-                               int M, int K, int N, void *dx_dev, void *dw_dev, void *db_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
-    const char *who = "adapt_int8_linear_backward";
-    if (int rc = int8_args(who, M, K, N, type)) return rc;
-    const size_t e = (size_t)adapt::element_size(type);
-    const bool want_dx = dx_dev && M > 0 && K > 0, want_dw = dw_dev && N > 0 && K > 0, want_db = db_dev && N > 0;
-    if (!want_dx && !want_dw && !want_db) return ADAPT_OK;
-    if (M > 0 && N > 0 && !dy_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL dy_dev", who);
-    if (want_dx && N > 0 && (!w_dev || !s_w_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL w_dev / s_w_dev", who);
-    if (want_dw && M > 0 && (!a_dev || !s_a_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL a_dev / s_a_dev", who);
-    for (const void *q : {dy_dev, (const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
-        if (off_by(q, e)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    for (const void *g : {(const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
-        if (g && (g == dy_dev || g == (const void *)a_dev || g == (const void *)w_dev))
-            return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
-    size_t need = 0;
-    if (int rc = adapt_int8_linear_backward_workspace(M, K, N, type, want_dx, want_dw, &need)) return rc;
-    if (need && (!workspace_dev || workspace_bytes < need || off_by(workspace_dev, 256)))
-        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, need);
-    const long long tx = (((long long)M + 31) / 32) * (((long long)K + 31) / 32), tw = (((long long)N + 31) / 32) * (((long long)K + 31) / 32);
-    if ((want_dx && tx >= INT8_TILES) || (want_dw && tw >= INT8_TILES)) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^34 gradients or more", who);
-    hipStream_t s = (hipStream_t)stream;
-    ADAPT_FOR_TYPE(type, E, {
-        const E::mem *const dy = static_cast<const E::mem *>(dy_dev);
-        if (want_dx) adapt::int8_gradient_kernel<E><<<(unsigned)tx, 256, 0, s>>>(dy, (size_t)N, 1, s_w_dev, w_dev, static_cast<E::mem *>(dx_dev), M, K, N);
-        if (want_dw) adapt::int8_gradient_kernel<E><<<(unsigned)tw, 256, 0, s>>>(dy, 1, (size_t)N, s_a_dev, a_dev, static_cast<E::mem *>(dw_dev), N, K, M);
-        if (want_db) adapt::int8_bias_grad_kernel<E><<<(unsigned)((N + 31ll) / 32), 256, 0, s>>>(dy, static_cast<E::mem *>(db_dev), M, N);
-    });
     HIP_TRY(hipGetLastError());
     return ADAPT_OK;
 }
