@@ -568,7 +568,7 @@ int adapt_embedding(const void *table_dev, int type, const void *tokens_dev, int
 /* Its gradient: dtable[v] = scale * sum over the places t with tok[t] = v of dy[t]; rows of tokens that do not occur, and row
  * padding_idx (-1: none), are zero; places whose token is padding_idx or lies outside [0, V) take no part (their dy is not read).
  * dtable_dev [V][D] of dy's element type, fully overwritten.  The places are sorted by token, so no sum depends on an order of
- * atomics.  workspace_dev: adapt_embedding_backward_workspace bytes. */
+ * atomics.  D <= 65535 * 64, else ADAPT_ERR_UNSUPPORTED.  workspace_dev: adapt_embedding_backward_workspace bytes. */
 int adapt_embedding_backward_workspace(size_t tokens, int V, int D, size_t *bytes);
 int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_dev, int token_bits, void *dtable_dev, size_t tokens, int V, int D, float scale,
                              int64_t padding_idx, void *workspace_dev, size_t workspace_bytes, void *stream);

@@ -131,7 +131,7 @@ GradPlan grad_plan(long long I, long long J, long long R, int P) {
 }
 int grad_pieces(int type) { return type == ADAPT_F32 ? 3 : 2; }
 
-size_t db_blocks(int M) { return ((size_t)M + adapt::GRAD_DB_ROWS - 1) / adapt::GRAD_DB_ROWS; }
+size_t db_blocks(int M) { return ((size_t)M + 63) / 64; }        // rows of partial sums of the bias gradient
 
 template <class E>
 void join(const float *part, int parts, size_t n, void *c, hipStream_t s) {
@@ -172,21 +172,21 @@ void gradients(const adapt::Int8Params &q, const void *dy_dev, void *dx, void *d
         }
         grad_product<E>(g, ws, q.M, q.K, dx, s);
     }
+    const size_t blocks = db_blocks(q.M);
     if (dw) {
         const GradPlan g = grad_plan(q.N, q.K, q.M, P);
         __bf16 *const b = reinterpret_cast<__bf16 *>(ws + g.b);
+        float *const part = db ? reinterpret_cast<float *>(ws + g.bytes) : nullptr;
         if (g.Rp) {
-            adapt::grad_split_columns_kernel<E, P><<<blocks64(g.Rp, q.N), 256, 0, s>>>(dy, q.s_a, a, q.M, q.N, g.Rp);
+            adapt::grad_split_columns_kernel<E, P, true><<<blocks64(g.Rp, q.N), 256, 0, s>>>(dy, q.s_a, a, part, q.M, q.N, g.Rp);
             adapt::grad_codes_kernel<P><<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.a, b, q.M, q.K, g.Rp);
         }
+        if (db) adapt::grad_bias_kernel<E><<<(unsigned)((q.N + 63) / 64), 1024, 0, s>>>(part, static_cast<typename E::mem *>(db), (int)blocks, q.N);
         grad_product<E>(g, ws, q.N, q.K, dw, s);
-    }
-    if (db) {
+    } else if (db) {
         float *const part = reinterpret_cast<float *>(ws);
-        const size_t blocks = db_blocks(q.M);
-        if (blocks) adapt::grad_bias_kernel<E><<<dim3((unsigned)blocks, (unsigned)((q.N + 63) / 64)), 256, 0, s>>>(dy, part, q.M, q.N);
-        else adapt::fill_u32_kernel<<<ew_grid((size_t)q.N), 256, 0, s>>>(reinterpret_cast<uint32_t *>(part), 0u, (size_t)q.N);
-        join<E>(part, blocks ? (int)blocks : 1, (size_t)q.N, db, s);
+        if (blocks) adapt::grad_split_columns_kernel<E, P, false><<<blocks64(q.M, q.N), 256, 0, s>>>(dy, nullptr, nullptr, part, q.M, q.N, 0);
+        adapt::grad_bias_kernel<E><<<(unsigned)((q.N + 63) / 64), 1024, 0, s>>>(part, static_cast<typename E::mem *>(db), (int)blocks, q.N);
     }
 }
 
@@ -220,14 +220,14 @@ int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want
     if (int rc = int8_args(who, M, K, N, type)) return rc;
     if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
     const int P = grad_pieces(type);
-    // (the bias gradient's partial sums are at home in any of it)
-    size_t need = round256((db_blocks(M) + 1) * (size_t)N * 4);
+    const size_t db = round256(db_blocks(M) * (size_t)N * 4);       // partial sums of the bias gradient: behind those of dw
+    size_t need = db;
     if (want_dx && M && K) {
         const size_t b = grad_plan(M, K, N, P).bytes;
         need = b > need ? b : need;
     }
     if (want_dw && N && K) {
-        const size_t b = grad_plan(N, K, M, P).bytes;
+        const size_t b = grad_plan(N, K, M, P).bytes + db;
         need = b > need ? b : need;
     }
     *bytes = need;

@@ -35,14 +35,14 @@ struct __attribute__((packed, aligned(sizeof(typename E::mem)))) Piece {
     typename E::mem v[N];
 };
 template <typename E, int N>
-__device__ __forceinline__ void load_piece(const typename E::mem *__restrict__ p, float (&out)[N]) {
+__device__ __forceinline__ void load_piece(const typename E::mem *p, float (&out)[N]) {
     Piece<E, N> t;
     __builtin_memcpy(&t, __builtin_assume_aligned(p, sizeof(typename E::mem)), sizeof(t));
 #pragma unroll
     for (int i = 0; i < N; ++i) out[i] = E::load(t.v[i]);
 }
 template <typename E, int N>
-__device__ __forceinline__ void store_piece(typename E::mem *__restrict__ p, const float (&in)[N]) {
+__device__ __forceinline__ void store_piece(typename E::mem *p, const float (&in)[N]) {
     Piece<E, N> t;
 #pragma unroll
     for (int i = 0; i < N; ++i) t.v[i] = E::store(in[i]);

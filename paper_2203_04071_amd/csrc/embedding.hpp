@@ -40,17 +40,19 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_kernel(const typename E
 
 // ---- the gradient: places sorted by token (stable), sums of runs of equal tokens
 //
-// Least significant digit first, EMB_BITS bits a pass; a workgroup owns EMB_TILE places: count digits, scan the counts, scatter.
+// Least significant digit first, up to EMB_BITS bits a pass, two launches a pass.  At most EMB_BLOCKS workgroups of 16 waves, each with a
+// contiguous share of the places, one digit per thread: count, then (every workgroup adds up the counts before its own) scatter.
 constexpr int EMB_BITS = 9;
-constexpr int EMB_TILE = 2048;
-constexpr int EMB_WAVES = EMB_THREADS / 64;
+constexpr int EMB_BLOCKS = 128;
+constexpr int EMB_SORT_THREADS = 1024;
+constexpr int EMB_WAVES = EMB_SORT_THREADS / 64;
 
 struct EmbedSort {
     const uint32_t *key_in, *at_in;     // nullptr in the first pass: keys come from the tokens, places are 0, 1, 2 ...
     uint32_t *key_out, *at_out;
-    uint32_t *counts;                   // [digit][workgroup]
-    uint8_t *used;                      // [V], set in the first pass
-    uint32_t T, V;
+    uint32_t *counts;                   // [workgroup][digit]
+    uint32_t *runs;                     // numbers of runs for embed_join_kernel (two), set to 0 in the first pass
+    uint32_t T, V, share;               // share: places of a workgroup, a multiple of EMB_SORT_THREADS
     int shift, bits;
     int64_t padding;                    // token without a gradient
 };
@@ -72,71 +74,61 @@ __device__ __forceinline__ uint64_t embed_peers(uint32_t digit, int bits, bool a
     return m;
 }
 
-// [wave][digit] counts of this workgroup's places; a wave owns a contiguous quarter of them
+// [wave][digit] counts of this workgroup's places; a wave owns a contiguous sixteenth of them
 template <typename Tok>
-__device__ __forceinline__ void embed_count(const EmbedSort &p, const Tok *__restrict__ tokens, uint32_t (*hist)[1 << EMB_BITS], bool mark) {
+__device__ __forceinline__ void embed_count(const EmbedSort &p, const Tok *__restrict__ tokens, uint32_t (*hist)[1 << EMB_BITS]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < EMB_WAVES << EMB_BITS; i += EMB_THREADS) hist[i >> EMB_BITS][i & ((1 << EMB_BITS) - 1)] = 0;
+    for (int i = threadIdx.x; i < EMB_WAVES << EMB_BITS; i += EMB_SORT_THREADS) hist[i >> EMB_BITS][i & ((1 << EMB_BITS) - 1)] = 0;
     __syncthreads();
-    const uint32_t from = blockIdx.x * EMB_TILE + wave * (EMB_TILE / EMB_WAVES);
-    for (int u = 0; u < EMB_TILE / EMB_WAVES; u += 64) {
+    const uint32_t per_wave = p.share / EMB_WAVES, from = blockIdx.x * p.share + wave * per_wave;
+    for (uint32_t u = 0; u < per_wave; u += 64) {
         const uint32_t i = from + u + lane;
-        if (i < p.T) {
-            const uint32_t key = embed_key(p, tokens, i);
-            if (mark && key < p.V) p.used[key] = 1;
-            atomicAdd(&hist[wave][(key >> p.shift) & ((1u << p.bits) - 1)], 1u);
-        }
+        if (i < p.T) atomicAdd(&hist[wave][(embed_key(p, tokens, i) >> p.shift) & ((1u << p.bits) - 1)], 1u);
     }
     __syncthreads();
 }
 
 template <typename Tok>
-__global__ __launch_bounds__(EMB_THREADS) void embed_count_kernel(const EmbedSort p, const Tok *__restrict__ tokens) {
+__global__ __launch_bounds__(EMB_SORT_THREADS) void embed_count_kernel(const EmbedSort p, const Tok *__restrict__ tokens) {
     __shared__ uint32_t hist[EMB_WAVES][1 << EMB_BITS];
-    embed_count(p, tokens, hist, p.key_in == nullptr);
-    for (int d = threadIdx.x; d < 1 << p.bits; d += EMB_THREADS) {
+    embed_count(p, tokens, hist);
+    const int d = threadIdx.x;
+    if (d < 1 << p.bits) {
         uint32_t s = 0;
 #pragma unroll
         for (int w = 0; w < EMB_WAVES; ++w) s += hist[w][d];
-        p.counts[(size_t)d * gridDim.x + blockIdx.x] = s;
+        p.counts[((size_t)blockIdx.x << p.bits) + d] = s;
     }
-}
-
-// exclusive sums of n counts in place; one workgroup
-__global__ __launch_bounds__(1024) void embed_scan_kernel(uint32_t *__restrict__ counts, uint32_t n) {
-    __shared__ uint32_t wave_sum[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t before = 0;
-    for (uint32_t base = 0; base < n; base += 1024) {
-        const uint32_t i = base + threadIdx.x;
-        const uint32_t own = i < n ? counts[i] : 0u;
-        uint32_t incl = own;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t o = __shfl_up(incl, off, 64);
-            if (lane >= off) incl += o;
-        }
-        if (lane == 63) wave_sum[wave] = incl;
-        __syncthreads();
-        uint32_t pre = before, total = 0;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) pre += wave_sum[w];
-            total += wave_sum[w];
-        }
-        if (i < n) counts[i] = pre + incl - own;
-        before += total;
-        __syncthreads();
-    }
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.runs[threadIdx.x] = 0;
 }
 
 template <typename Tok>
-__global__ __launch_bounds__(EMB_THREADS) void embed_scatter_kernel(const EmbedSort p, const Tok *__restrict__ tokens) {
+__global__ __launch_bounds__(EMB_SORT_THREADS) void embed_scatter_kernel(const EmbedSort p, const Tok *__restrict__ tokens) {
     __shared__ uint32_t hist[EMB_WAVES][1 << EMB_BITS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    embed_count(p, tokens, hist, false);
-    for (int d = threadIdx.x; d < 1 << p.bits; d += EMB_THREADS) {        // counts become the wave's next free place
-        uint32_t at = p.counts[(size_t)d * gridDim.x + blockIdx.x];
+    __shared__ uint32_t wave_sum[EMB_WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = threadIdx.x;
+    const bool mine = d < 1 << p.bits;
+    // places of digit d: in all workgroups, in those before this one
+    uint32_t all = 0, before = 0;
+    if (mine) {
+#pragma unroll 8
+        for (uint32_t b = 0; b < gridDim.x; ++b) {
+            const uint32_t c = p.counts[((size_t)b << p.bits) + d];
+            all += c;
+            before += b < blockIdx.x ? c : 0u;
+        }
+    }
+    uint32_t incl = all;                // and of the digits before it
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t o = __shfl_up(incl, off, 64);
+        if (lane >= off) incl += o;
+    }
+    if (lane == 63) wave_sum[wave] = incl;
+    embed_count(p, tokens, hist);       // (ends with a barrier)
+    if (mine) {                         // counts become the wave's next free place
+        uint32_t at = incl - all + before;
+        for (int w = 0; w < wave; ++w) at += wave_sum[w];
 #pragma unroll
         for (int w = 0; w < EMB_WAVES; ++w) {
             const uint32_t c = hist[w][d];
@@ -145,8 +137,8 @@ __global__ __launch_bounds__(EMB_THREADS) void embed_scatter_kernel(const EmbedS
         }
     }
     __syncthreads();
-    const uint32_t from = blockIdx.x * EMB_TILE + wave * (EMB_TILE / EMB_WAVES);
-    for (int u = 0; u < EMB_TILE / EMB_WAVES; u += 64) {
+    const uint32_t per_wave = p.share / EMB_WAVES, from = blockIdx.x * p.share + wave * per_wave;
+    for (uint32_t u = 0; u < per_wave; u += 64) {
         const uint32_t i = from + u + lane;
         const bool in = i < p.T;
         const uint32_t key = in ? embed_key(p, tokens, i) : 0u;
@@ -166,12 +158,16 @@ __global__ __launch_bounds__(EMB_THREADS) void embed_scatter_kernel(const EmbedS
     }
 }
 
+constexpr uint32_t EMB_LONG = 32;       // see embed_join_kernel
+
 // Sums.  The sorted places are cut into pieces of C, each summed by 2^lg lanes; a run of equal tokens inside a piece is finished there.
 // One that crosses pieces leaves a partial sum in every piece: `head` for the part at a piece's start that began earlier, `tail` for
-// the part at its end that goes on; embed_join_kernel adds them in order.
+// the part at its end that goes on; embed_join_kernel adds them in order.  Bounded by memory: dy is read once, the table written once.
 struct EmbedSum {
     const uint32_t *key, *at;
-    const uint8_t *used;
+    // pieces in whose tail a run begins that goes on, in any order: numbers of short and of long ones; short ones from the list's start
+    // on, long ones from its end back
+    uint32_t *runs, *run;
     float *head, *tail;                 // [pieces][D]
     uint32_t T, V, D, C, pieces;
     float scale;
@@ -179,18 +175,42 @@ struct EmbedSum {
     uint32_t sum_blocks;                // workgroups beyond these write the rows without a token
 };
 
+// Rows without a token: a lane looks for its row in the sorted keys, then the wave writes the rows that are not there.
+template <typename E>
+__device__ __forceinline__ void embed_empty_rows(const EmbedSum &p, typename E::mem *__restrict__ dtable) {
+    const uint32_t lane = threadIdx.x & 63, waves = (gridDim.x - p.sum_blocks) * (EMB_THREADS / 64);
+    constexpr int P = piece_len<E>;
+    const float zero[P] = {};
+    for (uint64_t v0 = ((uint64_t)(blockIdx.x - p.sum_blocks) * (EMB_THREADS / 64) + (threadIdx.x >> 6)) * 64; v0 < p.V; v0 += (uint64_t)waves * 64) {
+        const uint64_t v = v0 + lane;
+        uint32_t lo = 0, n = p.T;       // first place whose key is not below v
+        while (n > 0) {
+            const uint32_t half = n / 2;
+            const bool below = p.key[lo + half] < v;
+            lo = below ? lo + half + 1 : lo;
+            n = below ? n - half - 1 : half;
+        }
+        uint64_t absent = __ballot(v < p.V && (lo >= p.T || p.key[lo] != v));
+        while (absent) {
+            typename E::mem *const row = dtable + (size_t)(v0 + __builtin_ctzll(absent)) * p.D;
+            absent &= absent - 1;
+            for (uint32_t c = lane * P; c < p.D; c += 64 * P) {
+                if (c + P <= p.D) store_piece<E, P>(row + c, zero);
+                else
+                    for (uint32_t i = c; i < p.D; ++i) row[i] = E::store(0.0f);
+            }
+        }
+    }
+}
+
 template <typename E>
 __global__ __launch_bounds__(EMB_THREADS) void embed_sum_kernel(const EmbedSum p, const typename E::mem *__restrict__ dy, typename E::mem *__restrict__ dtable) {
     constexpr int P = piece_len<E>;
-    const uint32_t lane = threadIdx.x & ((1u << p.lg) - 1), per = EMB_THREADS >> p.lg;
     if (blockIdx.x >= p.sum_blocks) {
-        const uint32_t rows = (gridDim.x - p.sum_blocks) * per;
-        for (size_t v = (size_t)(blockIdx.x - p.sum_blocks) * per + (threadIdx.x >> p.lg); v < p.V; v += rows) {
-            if (p.used[v]) continue;
-            for (uint32_t c = lane; c < p.D; c += 1u << p.lg) dtable[v * p.D + c] = E::store(0.0f);
-        }
+        embed_empty_rows<E>(p, dtable);
         return;
     }
+    const uint32_t lane = threadIdx.x & ((1u << p.lg) - 1), per = EMB_THREADS >> p.lg;
     const uint32_t piece = blockIdx.x * per + (threadIdx.x >> p.lg);
     if (piece >= p.pieces) return;
     const uint32_t first = piece * p.C, last = min(first + p.C, p.T);       // (pieces cover T: first < T)
@@ -216,6 +236,15 @@ __global__ __launch_bounds__(EMB_THREADS) void embed_sum_kernel(const EmbedSum p
             if (open || next == key) {
                 float *const part = (open ? p.head : p.tail) + (size_t)piece * p.D + c;
                 for (int j = 0; j < len; ++j) part[j] = acc[j];
+                if (!open && c == 0) {
+                    const bool many = piece + EMB_LONG < p.pieces && p.key[(piece + EMB_LONG) * p.C] == key;
+                    const uint32_t at = atomicAdd(&p.runs[many], 1u);
+                    p.run[many ? p.pieces - 1 - at : at] = piece;
+                }
+            } else if (len == P) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) acc[j] *= p.scale;
+                store_piece<E, P>(dtable + (size_t)key * p.D + c, acc);
             } else {
                 for (int j = 0; j < len; ++j) dtable[(size_t)key * p.D + c + j] = E::store(acc[j] * p.scale);
             }
@@ -227,18 +256,59 @@ __global__ __launch_bounds__(EMB_THREADS) void embed_sum_kernel(const EmbedSum p
     }
 }
 
-// one workgroup per piece; it works if a run begins in the piece and goes on in the next
+// Runs that cross pieces, 64 columns each: a short one (up to EMB_LONG parts behind its first) is added by a wave, a long one by the sixteen waves of
+// a workgroup, a contiguous sixteenth of its parts each, whose sums the first wave adds in order.  (A run per workgroup of 256 columns, its
+// parts one after the other: 124 us for 65536 places of 1024 columns, a fifth of them one token.)
+constexpr unsigned EMB_LONG_BLOCKS = 32;
 template <typename E>
-__global__ __launch_bounds__(EMB_THREADS) void embed_join_kernel(const EmbedSum p, typename E::mem *__restrict__ dtable) {
-    const uint32_t piece = blockIdx.x, first = piece * p.C, end = first + p.C;
-    if (end >= p.T) return;
-    const uint32_t key = p.key[end - 1];
-    if (key >= p.V || p.key[end] != key) return;
-    if (p.key[first] == key && first > 0 && p.key[first - 1] == key) return;        // it began earlier
-    for (uint32_t c = threadIdx.x; c < p.D; c += EMB_THREADS) {
-        float s = p.tail[(size_t)piece * p.D + c];
-        for (uint32_t j = piece + 1; j < p.pieces && p.key[j * p.C] == key; ++j) s += p.head[(size_t)j * p.D + c];
-        dtable[(size_t)key * p.D + c] = E::store(s * p.scale);
+__global__ __launch_bounds__(1024) void embed_join_kernel(const EmbedSum p, typename E::mem *__restrict__ dtable) {
+    __shared__ float sum[16][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.y * 64 + lane;
+    // parts of the run that begins in the tail of `piece`: that tail, and the heads of the pieces whose first key is the run's
+    auto parts_of = [&](uint32_t piece, uint32_t key) {
+        uint32_t end = piece + 1, n = p.pieces - end;
+        while (n > 0) {
+            const uint32_t half = n / 2;
+            const bool in = p.key[(end + half) * p.C] == key;
+            end = in ? end + half + 1 : end;
+            n = in ? n - half - 1 : half;
+        }
+        return end - piece;
+    };
+    auto add = [&](uint32_t piece, uint32_t from, uint32_t to) {
+        float s = 0.0f;
+        uint32_t j = from;
+        for (; j + 8 <= to; j += 8) {
+            float t[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t[u] = (j + u == 0 ? p.tail : p.head)[(size_t)(piece + j + u) * p.D + c];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += t[u];
+        }
+        for (; j < to; ++j) s += (j == 0 ? p.tail : p.head)[(size_t)(piece + j) * p.D + c];
+        return s;
+    };
+    if (blockIdx.x < EMB_LONG_BLOCKS) {
+        const uint32_t runs = p.runs[1];
+        for (uint32_t r = blockIdx.x; r < runs; r += EMB_LONG_BLOCKS) {
+            const uint32_t piece = p.run[p.pieces - 1 - r], key = p.key[(piece + 1) * p.C], parts = parts_of(piece, key);
+            const uint32_t share = (parts + 15) / 16, from = min(wave * share, parts), to = min(from + share, parts);
+            float s = c < p.D ? add(piece, from, to) : 0.0f;
+            sum[wave][lane] = s;
+            __syncthreads();
+            if (wave == 0 && c < p.D) {
+#pragma unroll
+                for (int w = 1; w < 16; ++w) s += sum[w][lane];
+                dtable[(size_t)key * p.D + c] = E::store(s * p.scale);
+            }
+            __syncthreads();
+        }
+    } else if (c < p.D) {
+        const uint32_t runs = p.runs[0], waves = (gridDim.x - EMB_LONG_BLOCKS) * 16;
+        for (uint32_t r = (blockIdx.x - EMB_LONG_BLOCKS) * 16 + wave; r < runs; r += waves) {
+            const uint32_t piece = p.run[r], key = p.key[(piece + 1) * p.C];
+            dtable[(size_t)key * p.D + c] = E::store(add(piece, 0, parts_of(piece, key)) * p.scale);
+        }
     }
 }
 

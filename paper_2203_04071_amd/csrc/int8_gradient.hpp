@@ -61,12 +61,10 @@ __global__ __launch_bounds__(256) void grad_split_rows_kernel(const typename E::
 
 // 64 x 64 elements src[r][c] come out as out[c][z][r], padded with zeros to Rp rows: the transposed operands.  A workgroup holds the block in
 // LDS as floats; lanes read along c and write along r, 16 bytes a lane.
-template <typename Load, typename Write>
-__device__ __forceinline__ void grad_transpose(int R, int C, Load &&load, Write &&write) {
-    __shared__ float tile[64][65];
+constexpr int GRAD_LD = 65;
+template <typename Write>
+__device__ __forceinline__ void grad_transposed(const float (&tile)[64][GRAD_LD], int C, Write &&write) {
     const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-    load(tile, r0, c0);
-    __syncthreads();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int c = (threadIdx.x >> 3) + 32 * u, r = (threadIdx.x & 7) * 8;
@@ -78,74 +76,110 @@ __device__ __forceinline__ void grad_transpose(int R, int C, Load &&load, Write 
     }
 }
 
-// out[n][z][m] = piece z of dy[m][n] * s[m]
-template <typename E, int P>
+// out[n][z][m] = piece z of dy[m][n] * s[m] (PIECES), and on the way part[block][n] = sum of dy[m][n] over the block's 64 rows (part != nullptr).
+// Without PIECES the sums alone, the same ones.
+template <typename E, int P, bool PIECES>
 __global__ __launch_bounds__(256) void grad_split_columns_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, __bf16 *__restrict__ out,
-                                                                 int M, int N, int Mp) {
-    grad_transpose(
-        M, N,
-        [&](float(&tile)[64][65], int r0, int c0) {
-            const int c = (threadIdx.x & 15) * 4;
+                                                                 float *__restrict__ part, int M, int N, int Mp) {
+    __shared__ float tile[64][GRAD_LD];
+    __shared__ float column[16][64];
+    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, c = (threadIdx.x & 15) * 4, n = c0 + c;
+    float t[4][4], sum[4] = {};
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int r = (threadIdx.x >> 4) + 16 * u, m = r0 + r, n = c0 + c;
-                float t[4] = {};
-                if (m < M) {
-                    const typename E::mem *const at = dy + (size_t)m * (size_t)N + n;
-                    if (n + 4 <= N) load_piece<E, 4>(at, t);
-                    else
+    for (int u = 0; u < 4; ++u) {
+        const int m = r0 + (threadIdx.x >> 4) + 16 * u;
+        const typename E::mem *const at = dy + (size_t)m * (size_t)N + n;
+        if (m < M && n + 4 <= N) {
+            load_piece<E, 4>(at, t[u]);
+        } else {
 #pragma unroll
-                        for (int j = 0; j < 3; ++j)
-                            if (n + j < N) t[j] = E::load(at[j]);
-                    const float sm = s[m];
+            for (int j = 0; j < 4; ++j) t[u][j] = m < M && n + j < N ? E::load(at[j]) : 0.0f;
+        }
+    }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) t[j] *= sm;
-                    if (n + 4 > N)          // (a scale of infinity times nothing)
+    for (int u = 0; u < 4; ++u) {
+        const int r = (threadIdx.x >> 4) + 16 * u, m = r0 + r;
+        const float sm = PIECES && m < M ? s[m] : 0.0f;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) t[j] = n + j < N ? t[j] : 0.0f;
-                }
+        for (int j = 0; j < 4; ++j) {
+            sum[j] += t[u][j];
+            if constexpr (PIECES) tile[r][c + j] = m < M && n + j < N ? t[u][j] * sm : 0.0f;
+        }
+    }
+    if (part)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) tile[r][c + j] = t[j];
-            }
-        },
-        [&](int n, int m, const float(&t)[8]) {
+        for (int j = 0; j < 4; ++j) column[threadIdx.x >> 4][c + j] = sum[j];
+    __syncthreads();
+    if constexpr (PIECES)
+        grad_transposed(tile, N, [&](int col, int row, const float(&e)[8]) {
             bf16x8_t v[P];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 __bf16 q[P];
-                split_pieces<P>(t[j], q);
+                split_pieces<P>(e[j], q);
 #pragma unroll
                 for (int z = 0; z < P; ++z) v[z][j] = q[z];
             }
 #pragma unroll
-            for (int z = 0; z < P; ++z) *reinterpret_cast<bf16x8_t *>(out + ((size_t)n * P + z) * (size_t)Mp + m) = v[z];
+            for (int z = 0; z < P; ++z) *reinterpret_cast<bf16x8_t *>(out + ((size_t)col * P + z) * (size_t)Mp + row) = v[z];
         });
+    if (part && threadIdx.x < 64 && c0 + (int)threadIdx.x < N) {
+        float total = column[0][threadIdx.x];
+#pragma unroll
+        for (int g = 1; g < 16; ++g) total += column[g][threadIdx.x];
+        part[(size_t)blockIdx.x * (size_t)N + c0 + threadIdx.x] = total;
+    }
+}
+
+// db[n] = the sum of the blocks' sums: 64 columns per workgroup, sixteen waves with every sixteenth block each
+template <typename E>
+__global__ __launch_bounds__(1024) void grad_bias_kernel(const float *__restrict__ part, typename E::mem *__restrict__ db, int blocks, int N) {
+    __shared__ float sum[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (n < N) {
+#pragma unroll 8
+        for (int b = wave; b < blocks; b += 16) s += part[(size_t)b * (size_t)N + n];
+    }
+    sum[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && n < N) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += sum[w][lane];
+        db[n] = E::store(s);
+    }
 }
 
 // out[c][z][r] = q[r][c] * 2^(-8 (P - 1 - z))
 template <int P>
 __global__ __launch_bounds__(256) void grad_codes_kernel(const int8_t *__restrict__ q, __bf16 *__restrict__ out, int R, int C, int Rp) {
-    grad_transpose(
-        R, C,
-        [&](float(&tile)[64][65], int r0, int c0) {
-            const int c = (threadIdx.x & 15) * 4;
+    __shared__ float tile[64][GRAD_LD];
+    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int rl = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16, r = r0 + rl;
+    i32x4_t v = {0, 0, 0, 0};
+    if (r < R) {
+        const int8_t *const at = q + (size_t)r * (size_t)C + c0 + c;
+        if (c0 + c + 16 <= C) {
+            __builtin_memcpy(&v, at, 16);
+        } else {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int rl = (threadIdx.x >> 4) + 16 * u, r = r0 + rl;
+            for (int j = 0; j < 15; ++j)
+                if (c0 + c + j < C) v[j / 4] |= (int)((uint32_t)(uint8_t)at[j] << (8 * (j % 4)));
+        }
+    }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) tile[rl][c + j] = r < R && c0 + c + j < C ? (float)q[(size_t)r * (size_t)C + c0 + c + j] : 0.0f;
-            }
-        },
-        [&](int c, int r, const float(&t)[8]) {
+    for (int j = 0; j < 16; ++j) tile[rl][c + j] = (float)(int8_t)(v[j / 4] >> (8 * (j % 4)));
+    __syncthreads();
+    grad_transposed(tile, C, [&](int col, int row, const float(&t)[8]) {
 #pragma unroll
-            for (int z = 0; z < P; ++z) {
-                const float f = z == P - 1 ? 1.0f : (z == P - 2 ? 0x1p-8f : 0x1p-16f);
-                bf16x8_t v;
+        for (int z = 0; z < P; ++z) {
+            const float f = z == P - 1 ? 1.0f : (z == P - 2 ? 0x1p-8f : 0x1p-16f);
+            bf16x8_t b;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (__bf16)(t[j] * f);
-                *reinterpret_cast<bf16x8_t *>(out + ((size_t)c * P + z) * (size_t)Rp + r) = v;
-            }
-        });
+            for (int j = 0; j < 8; ++j) b[j] = (__bf16)(t[j] * f);
+            *reinterpret_cast<bf16x8_t *>(out + ((size_t)col * P + z) * (size_t)Rp + row) = b;
+        }
+    });
 }
 
 // c[i] = part[0][i] + part[1][i] + ... in that order, rounded to E
@@ -170,28 +204,6 @@ __global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict_
             }
         }
     }
-}
-
-// db[n] = sum_m dy[m][n]: a workgroup adds GRAD_DB_ROWS rows of 64 columns (four threads per column, every fourth row each) to part[block][n];
-// grad_join_kernel adds those
-constexpr int GRAD_DB_ROWS = 128;
-template <typename E>
-__global__ __launch_bounds__(256) void grad_bias_kernel(const typename E::mem *__restrict__ dy, float *__restrict__ part, int M, int N) {
-    __shared__ float p[4][64];
-    const int c = threadIdx.x & 63, ph = threadIdx.x >> 6, n = blockIdx.y * 64 + c, m0 = blockIdx.x * GRAD_DB_ROWS;
-    float s = 0.0f;
-    if (n < N) {
-        const typename E::mem *const at = dy + (size_t)m0 * (size_t)N + n;
-        if (m0 + GRAD_DB_ROWS <= M) {
-#pragma unroll 8
-            for (int r = ph; r < GRAD_DB_ROWS; r += 4) s += E::load(at[(size_t)r * (size_t)N]);
-        } else {
-            for (int r = ph; m0 + r < M; r += 4) s += E::load(at[(size_t)r * (size_t)N]);
-        }
-    }
-    p[ph][c] = s;
-    __syncthreads();
-    if (ph == 0 && n < N) part[(size_t)blockIdx.x * N + n] = ((p[0][c] + p[1][c]) + p[2][c]) + p[3][c];
 }
 
 }  // namespace adapt

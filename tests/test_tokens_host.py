@@ -137,7 +137,7 @@ def test_workspaces_grow_with_the_call(lib):
         return n.value
     for V, D in ((1, 1), (511, 16), (512, 33), (50000, 1024), (1 << 30, 8)):
         sizes = [emb(T, V, D) for T in (0, 1, 31, 32, 33, 2047, 2048, 2049, 65536, 1 << 20)]
-        assert sizes == sorted(sizes) and sizes[0] >= V
+        assert sizes == sorted(sizes) and sizes[-1] > sizes[0]
 
 
 # ---- the oracle itself
