@@ -43,7 +43,8 @@ EmbedPlan embed_plan(size_t T, int V, int D) {
     e.T = (uint32_t)T;
     e.V = (uint32_t)V;
     e.D = (uint32_t)D;
-    e.C = 32;
+    // (few places: short pieces, for their latency; many: long ones, for the partial sums that are written and read again)
+    e.C = e.T <= 8192 ? 8 : (e.T <= 16384 ? 16 : (e.T <= 32768 ? 32 : 64));
     e.pieces = (e.T + e.C - 1) / e.C;
     e.share = (e.T + adapt::EMB_BLOCKS - 1) / adapt::EMB_BLOCKS;
     e.share = (e.share + adapt::EMB_SORT_THREADS - 1) / adapt::EMB_SORT_THREADS * adapt::EMB_SORT_THREADS;
@@ -85,6 +86,14 @@ void embed_sort(const EmbedPlan &e, const Tok *tokens, char *ws, int64_t padding
     p.share = e.share;
     p.bits = e.bits;
     p.padding = padding;
+    if (e.T <= adapt::EMB_SMALL) {
+        p.key_out = reinterpret_cast<uint32_t *>(ws);
+        p.at_out = reinterpret_cast<uint32_t *>(ws + e.list);
+        adapt::embed_sort_small_kernel<<<1, adapt::EMB_SORT_THREADS, 0, s>>>(p, tokens, e.passes);
+        *key = p.key_out;
+        *at = p.at_out;
+        return;
+    }
     for (int pass = 0; pass < e.passes; ++pass) {
         char *const to = ws + (pass & 1 ? 2 * e.list : 0);
         p.key_out = reinterpret_cast<uint32_t *>(to);
@@ -218,7 +227,7 @@ int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_de
         p.lg = lanes_lg<E>(D);
         const unsigned per = (unsigned)(adapt::EMB_THREADS >> p.lg);
         p.sum_blocks = (pl.pieces + per - 1) / per;
-        const unsigned zero_blocks = cap_grid(((size_t)V + 255) / 256, 4096);
+        const unsigned zero_blocks = cap_grid(((size_t)V + 4 * adapt::EMB_ZERO_ROWS - 1) / (4 * adapt::EMB_ZERO_ROWS), 4096);
         adapt::embed_sum_kernel<E><<<p.sum_blocks + zero_blocks, adapt::EMB_THREADS, 0, s>>>(p, static_cast<const E::mem *>(dy_dev), static_cast<E::mem *>(dtable_dev));
         if (pl.pieces > 1)
             adapt::embed_join_kernel<E><<<dim3(adapt::EMB_LONG_BLOCKS + cap_grid((pl.pieces + 15) / 16, 64), ((unsigned)D + 63) / 64), 1024, 0, s>>>(p, static_cast<E::mem *>(dtable_dev));
