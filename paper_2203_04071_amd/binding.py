@@ -850,54 +850,66 @@ def adapt_relu_backward_f32(dy, y, out=None, stream=None):
 
 ELEMENT_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
+_here = torch._C._cuda_getDevice
 
 
-def _element(t):
-    if t.dtype not in ELEMENT_TYPES:
-        raise TypeError(f"expected float32, float16 or bfloat16, got {t.dtype}")
-    return ELEMENT_TYPES[t.dtype]
+def _element(dtype):
+    e = ELEMENT_TYPES.get(dtype)
+    if e is None:
+        raise TypeError(f"expected float32, float16 or bfloat16, got {dtype}")
+    return e
 
 
-def _shape(what, t, want):
-    if tuple(t.shape) != tuple(want):
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(want)}")
+def _arg(what, t, dtype, shape, here):
+    """The tensor's address, if it is what the call needs: the library launches on the current device and takes dense rows.  (One test
+    of everything: a call's arguments took half as long to check as the launch itself.)"""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == here and t.is_contiguous():
+        return t.data_ptr()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a tensor, got {type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not (t.is_cuda and t.is_contiguous()):
+        raise TypeError(f"{what}: expected a contiguous CUDA tensor")
+    if t.get_device() != here:
+        raise ValueError(f"{what} is on cuda:{t.get_device()}, but the current device is cuda:{here}")
+    return t.data_ptr()
 
 
-def _here(*tensors):
-    """The library launches on the current device: tensors of another one would be read from the wrong side."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != here:
-            raise ValueError(f"tensor on cuda:{t.device.index}, but the current device is cuda:{here}")
+def _raw_stream(stream, here):
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
 
 
-def _new(stream, shape, dtype):
+def _new(stream, like, shape, dtype):
     """Memory of `stream` (a block given back on the current stream may still be in use there)."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _workspace(workspace, need, stream):
+def _workspace(workspace, need, stream, like, here):
     """The caller's uint8 tensor if it is large enough, else a new one, which the calling function holds until its kernels are enqueued."""
+    if workspace is not None:
+        _arg("workspace", workspace, torch.uint8, (workspace.numel(),), here)
     if workspace is None or workspace.numel() < need:
-        workspace = _new(stream, (need,), torch.uint8)
+        workspace = _new(stream, like, (need,), torch.uint8)
     return workspace
 
 
 def adapt_quantize_tokens(x, bits: int = 8, out=None, scales=None, stream=None):
     """x [tokens][cols] -> (int8 codes [tokens][cols], fp32 scale per token)."""
     tokens, cols = x.shape
-    _here(x, out, scales)
+    here = _here()
+    px = _arg("x", x, x.dtype, (tokens, cols), here)
     if out is None:
-        out = _new(stream, (tokens, cols), torch.int8)
+        out = _new(stream, x, (tokens, cols), torch.int8)
     if scales is None:
-        scales = _new(stream, (tokens,), torch.float32)
-    _shape("out", out, (tokens, cols))
-    _shape("scales", scales, (tokens,))
-    _chk(load().adapt_quantize_tokens(_ptr(x), _element(x), _ptr(out, torch.int8), _ptr(scales, torch.float32), tokens, cols, bits,
-                                      _stream(stream)))
+        scales = _new(stream, x, (tokens,), torch.float32)
+    _chk(load().adapt_quantize_tokens(px, _element(x.dtype), _arg("out", out, torch.int8, (tokens, cols), here),
+                                      _arg("scales", scales, torch.float32, (tokens,), here), tokens, cols, bits, _raw_stream(stream, here)))
     return out, scales
 
 
@@ -905,17 +917,16 @@ def adapt_int8_linear(a, s_a, w, s_w, bias=None, act: int = 0, dtype=torch.float
     """Codes a [M][K], w [N][K] with scales s_a [M], s_w [N] -> act(a w^T s_a s_w + bias) [M][N] of `dtype` (out's, if given)."""
     M, K = a.shape
     N = w.shape[0]
-    _shape("w", w, (N, K))
-    _shape("s_a", s_a, (M,))
-    _shape("s_w", s_w, (N,))
-    if bias is not None:
-        _shape("bias", bias, (N,))
-    _here(a, s_a, w, s_w, bias, out)
+    here = _here()
+    pa = _arg("a", a, torch.int8, (M, K), here)
     if out is None:
-        out = _new(stream, (M, N), dtype)
-    _shape("out", out, (M, N))
-    _chk(load().adapt_int8_linear(_ptr(a, torch.int8), _ptr(s_a, torch.float32), _ptr(w, torch.int8), _ptr(s_w, torch.float32),
-                                  _ptr(bias, torch.float32), act, _ptr(out), _element(out), M, K, N, _stream(stream)))
+        out = _new(stream, a, (M, N), dtype)
+    else:
+        dtype = out.dtype
+    _chk(load().adapt_int8_linear(pa, _arg("s_a", s_a, torch.float32, (M,), here), _arg("w", w, torch.int8, (N, K), here),
+                                  _arg("s_w", s_w, torch.float32, (N,), here),
+                                  None if bias is None else _arg("bias", bias, torch.float32, (N,), here), act,
+                                  _arg("out", out, dtype, (M, N), here), _element(dtype), M, K, N, _raw_stream(stream, here)))
     return out
 
 
@@ -924,37 +935,40 @@ def adapt_int8_linear_backward(dy, a, s_a, w, s_w, want=("dx", "dw", "db"), work
     workspace: a uint8 device tensor to reuse (allocated here when None or too small)."""
     M, N = dy.shape
     K = w.shape[1]
-    _shape("a", a, (M, K))
-    _shape("w", w, (N, K))
-    _shape("s_a", s_a, (M,))
-    _shape("s_w", s_w, (N,))
-    _here(dy, a, s_a, w, s_w, workspace)
+    here = _here()
+    e = _element(dy.dtype)
+    operands = (_arg("a", a, torch.int8, (M, K), here), _arg("s_a", s_a, torch.float32, (M,), here),
+                _arg("w", w, torch.int8, (N, K), here), _arg("s_w", s_w, torch.float32, (N,), here))
+    pdy = _arg("dy", dy, dy.dtype, (M, N), here)
     need = ctypes.c_size_t(0)
-    _chk(load().adapt_int8_linear_backward_workspace(M, K, N, _element(dy), int("dx" in want), int("dw" in want), ctypes.byref(need)))
-    ws = _workspace(workspace, need.value, stream)
-    dx = _new(stream, (M, K), dy.dtype) if "dx" in want else None
-    dw = _new(stream, (N, K), dy.dtype) if "dw" in want else None
-    db = _new(stream, (N,), dy.dtype) if "db" in want else None
-    _chk(load().adapt_int8_linear_backward(_ptr(dy), _element(dy), _ptr(a, torch.int8), _ptr(s_a, torch.float32), _ptr(w, torch.int8),
-                                           _ptr(s_w, torch.float32), M, K, N, _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws, torch.uint8), ws.numel(), _stream(stream)))
+    _chk(load().adapt_int8_linear_backward_workspace(M, K, N, e, int("dx" in want), int("dw" in want), ctypes.byref(need)))
+    ws = _workspace(workspace, need.value, stream, dy, here)
+    dx = _new(stream, dy, (M, K), dy.dtype) if "dx" in want else None
+    dw = _new(stream, dy, (N, K), dy.dtype) if "dw" in want else None
+    db = _new(stream, dy, (N,), dy.dtype) if "db" in want else None
+    _chk(load().adapt_int8_linear_backward(pdy, e, *operands, M, K, N, *(None if t is None else t.data_ptr() for t in (dx, dw, db)),
+                                           ws.data_ptr(), ws.numel(), _raw_stream(stream, here)))
     return dx, dw, db
 
 
-def _tokens(tokens):
-    if tokens.dtype not in TOKEN_BITS:
+def _tokens(tokens, here):
+    bits = TOKEN_BITS.get(tokens.dtype)
+    if bits is None:
         raise TypeError(f"expected int32 or int64 tokens, got {tokens.dtype}")
-    return _ptr(tokens), TOKEN_BITS[tokens.dtype]
+    return _arg("tokens", tokens, tokens.dtype, tokens.shape, here), bits
 
 
 def adapt_embedding(table, tokens, scale: float = 1.0, out=None, stream=None):
     """Rows of table [V][D] for tokens of any shape, times scale; a token outside [0, V) gives zeros."""
     V, D = table.shape
-    _here(table, tokens, out)
+    here = _here()
+    tok, tok_bits = _tokens(tokens, here)
+    pt = _arg("table", table, table.dtype, (V, D), here)
+    shape = (*tokens.shape, D)
     if out is None:
-        out = _new(stream, tuple(tokens.shape) + (D,), table.dtype)
-    _shape("out", out, tuple(tokens.shape) + (D,))
-    tok, tok_bits = _tokens(tokens)
-    _chk(load().adapt_embedding(_ptr(table), _element(table), tok, tok_bits, _ptr(out, table.dtype), tokens.numel(), V, D, float(scale), _stream(stream)))
+        out = _new(stream, table, shape, table.dtype)
+    _chk(load().adapt_embedding(pt, _element(table.dtype), tok, tok_bits, _arg("out", out, table.dtype, shape, here), tokens.numel(), V, D,
+                                scale, _raw_stream(stream, here)))
     return out
 
 
@@ -962,28 +976,29 @@ def adapt_embedding_backward(dy, tokens, V: int, scale: float = 1.0, padding_idx
     """dy [...][D] at tokens [...] -> gradient [V][D] of the table, of dy's type.
     workspace: a uint8 device tensor to reuse (allocated here when None or too small)."""
     D = dy.shape[-1]
-    _shape("dy", dy, tuple(tokens.shape) + (D,))
-    _here(dy, tokens, out, workspace)
+    here = _here()
+    tok, tok_bits = _tokens(tokens, here)
+    pdy = _arg("dy", dy, dy.dtype, (*tokens.shape, D), here)
+    e = _element(dy.dtype)
     if out is None:
-        out = _new(stream, (V, D), dy.dtype)
-    _shape("out", out, (V, D))
+        out = _new(stream, dy, (V, D), dy.dtype)
+    pout = _arg("out", out, dy.dtype, (V, D), here)
     need = ctypes.c_size_t(0)
     _chk(load().adapt_embedding_backward_workspace(tokens.numel(), V, D, ctypes.byref(need)))
-    ws = _workspace(workspace, need.value, stream)
-    tok, tok_bits = _tokens(tokens)
-    _chk(load().adapt_embedding_backward(_ptr(dy), _element(dy), tok, tok_bits, _ptr(out, dy.dtype), tokens.numel(), V, D, float(scale), padding_idx,
-                                         _ptr(ws, torch.uint8), ws.numel(), _stream(stream)))
+    ws = _workspace(workspace, need.value, stream, dy, here)
+    _chk(load().adapt_embedding_backward(pdy, e, tok, tok_bits, pout, tokens.numel(), V, D, scale, padding_idx, ws.data_ptr(), ws.numel(),
+                                         _raw_stream(stream, here)))
     return out
 
 
 def _dropout(call, x, p, seed, offset, step, out, stream):
-    _here(x, step, out)
+    here = _here()
+    px = _arg("x", x, x.dtype, x.shape, here)
+    e = _element(x.dtype)
     if out is None:
-        out = _new(stream, tuple(x.shape), x.dtype)
-    _shape("out", out, tuple(x.shape))
-    if step is not None and step.numel() != 1:
-        raise ValueError("step must hold one int64")
-    _chk(call(_ptr(x), _ptr(out, x.dtype), _element(x), x.numel(), float(p), int(seed), int(offset), _ptr(step, torch.int64), _stream(stream)))
+        out = _new(stream, x, x.shape, x.dtype)
+    _chk(call(px, _arg("out", out, x.dtype, x.shape, here), e, x.numel(), p, seed, offset,
+              None if step is None else _arg("step", step, torch.int64, (1,), here), _raw_stream(stream, here)))
     return out
 
 
