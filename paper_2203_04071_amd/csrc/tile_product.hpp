@@ -91,8 +91,8 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_i, uint32_t 
 // DMA: rows are multiples of 16 bytes and 16-byte aligned; pieces go from memory to LDS without registers, requested NB - 1 stages ahead, one
 // barrier a stage.  8192 x 8192 x 8192 int8 -> bf16 480 us, 2.3 POP/s; on all compute units the clock falls to 1.8 GHz, at which the matrix
 // pipe is busy for 3/4 of the time (alone on the chip a workgroup keeps it busy for 83 %).
-// Otherwise (rows of any length and address): pieces pass through registers, which also put zeros behind a row's end; the next stage's
-// are requested before this one is multiplied.  1111 x 777 -> 999 10.5 us.
+// Otherwise (rows of any length and address): pieces pass through registers, three stages ahead, which also put zeros behind a row's end.  Bounded by
+// the memory pipe, which takes longer over 16 bytes at an odd address: 1111 x 4096 -> 999 21 us against 14, 4095 26 us.
 template <class Op, class E, int TM, int TN, int SB, int NB, bool DMA, bool TANH = false>
 __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TileParams p) {
     const int k0 = (int)blockIdx.y * p.Kb_split, Kb = min(p.Kb - k0, p.Kb_split);
@@ -232,42 +232,66 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
             }
         }
     } else {
-        // (the stages that are whole for every row without a condition, so that their requests are on their way together)
-        i32x4_t reg[NQ];
-        auto fetch = [&](int s) {
-            if (s < full) {
+        // Three stages are on their way in registers.  Requests are made without a condition, so that they overlap: one behind a row's end
+        // fetches the row's last 16 bytes, which are moved down (or out) when they go to LDS.
+        i32x4_t reg[3][NQ];
+        auto fetch = [&](i32x4_t(&to)[NQ], int s) {
+            const int k = min(s * SB + piece16, Kb - 16);
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) __builtin_memcpy(&reg[q], (q < QA ? abase : bbase) + voff[q] + s * SB + piece16, 16);
-            } else {
+            for (int q = 0; q < NQ; ++q) __builtin_memcpy(&to[q], (q < QA ? abase : bbase) + (voff[q] + (uint32_t)k), 16);
+        };
+        auto stash = [&](i32x4_t(&from)[NQ], int s) {
+            if (s >= full) {
+                const int down = s * SB + piece16 - (Kb - 16);
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) reg[q] = row_piece((q < QA ? abase : bbase) + voff[q], s * SB + piece16, Kb);
+                for (int q = 0; q < NQ; ++q) {
+                    unsigned __int128 t;
+                    __builtin_memcpy(&t, &from[q], 16);
+                    t = down < 16 ? t >> (8 * max(down, 0)) : 0;
+                    __builtin_memcpy(&from[q], &t, 16);
+                }
             }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) *reinterpret_cast<i32x4_t *>(lds + (s & 1) * STAGE + place(q) + lane * 16) = from[q];
         };
-        auto stash = [&](int buf) {
+        // (a stage's fragments are requested together: one LDS latency a stage instead of one a step)
+        auto multiply = [&](int s) {
+            i32x4_t g[STEPS][NR];
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) *reinterpret_cast<i32x4_t *>(lds + buf * STAGE + place(q) + lane * 16) = reg[q];
+            for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) read1(g[st], r, s & 1, st);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                for (int k = 0; k < NS; ++k) acc[k / BJ][k % BJ] = Op::mfma(g[st][BI + k % BJ], g[st][k / BJ], acc[k / BJ][k % BJ]);
         };
-        auto multiply = [&](int buf) {
-#pragma unroll
-            for (int r = 0; r < NR; ++r) read1(f[0], r, buf, 0);
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                if (st + 1 < STEPS)
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) read1(f[(st + 1) & 1], r, buf, st + 1);
-#pragma unroll
-                for (int k = 0; k < NS; ++k) acc[k / BJ][k % BJ] = Op::mfma(f[st & 1][BI + k % BJ], f[st & 1][k / BJ], acc[k / BJ][k % BJ]);
+        // stage s, whose registers are free; `next` holds stage s + 1
+        auto stage = [&](i32x4_t(&own)[NQ], i32x4_t(&next)[NQ], int s) {
+            fetch(own, s + 3);
+            multiply(s);
+            stash(next, s + 1);
+            __syncthreads();
+        };
+        if (Kb >= 16) {
+            fetch(reg[0], 0);
+            fetch(reg[1], 1);
+            fetch(reg[2], 2);
+            stash(reg[0], 0);
+            __syncthreads();
+            for (int s = 0; s < total; s += 3) {        // (stages behind the last are zeros)
+                stage(reg[0], reg[1], s);
+                if (s + 1 >= total) break;
+                stage(reg[1], reg[2], s + 1);
+                if (s + 2 >= total) break;
+                stage(reg[2], reg[0], s + 2);
             }
-        };
-        if (total > 0) {
-            fetch(0);
-            stash(0);
-        }
-        __syncthreads();
-        for (int s = 0; s < total; ++s) {
-            if (s + 1 < total) fetch(s + 1);
-            multiply(s & 1);
-            if (s + 1 < total) stash((s + 1) & 1);
+        } else if (Kb > 0) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) *reinterpret_cast<i32x4_t *>(lds + place(q) + lane * 16) = row_piece((q < QA ? abase : bbase) + voff[q], piece16, Kb);
+            __syncthreads();
+            multiply(0);
             __syncthreads();
         }
     }
