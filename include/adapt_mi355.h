@@ -529,9 +529,9 @@ int adapt_sgd_step_f32(float *w_dev, const float *g_dev, size_t n, float lr, voi
  * ---------------------------------------------------------------------------------------------- */
 
 /* Quantiser of Sec. III-A with the range taken from every row ("token") of x [tokens][cols] itself:
- *     scales[t] = max_c |x[t][c]| / Q  (NaN skipped; 0 for a row of zeros or no columns),   Q = 2^(bits-1) - 1,
+ *     scales[t] = max_c |x[t][c]| * (1 / Q)  (NaN skipped; 0 for a row of zeros or no columns),   Q = 2^(bits-1) - 1, 1 / Q rounded to fp32,
  *     q[t][c] = clamp(round_half_even(x[t][c] / scales[t]), -Q, Q);   0 where x is NaN and where scales[t] = 0
- * in fp32 (IEEE divisions), 2 <= bits <= 8.  A row that holds an infinity gets scales[t] = inf and codes 0: its products with
+ * in fp32 (the codes by IEEE division: those of adapt_quantize_rows_f32 with these scales), 2 <= bits <= 8.  A row that holds an infinity gets scales[t] = inf and codes 0: its products with
  * adapt_int8_linear are NaN.  q_dev [tokens][cols] int8, scales_dev [tokens] fp32. */
 int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *scales_dev, size_t tokens, size_t cols, int bits,
                           void *stream);

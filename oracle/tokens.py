@@ -7,11 +7,11 @@ import numpy as np
 
 
 def quantize_tokens(x, bits):
-    """x float [M][K] -> (int8 codes, fp32 scales); every quotient an IEEE fp32 division."""
+    """x float [M][K] -> (int8 codes, fp32 scales): the scale a product with the rounded 1 / Q, every code by an IEEE fp32 division."""
     x = np.asarray(x, dtype=np.float32)
     q_max = np.float32((1 << (bits - 1)) - 1)
     mag = np.where(np.isnan(x), np.float32(0), np.abs(x))
-    s = (mag.max(axis=1) if x.shape[1] else np.zeros(x.shape[0], np.float32)) / q_max
+    s = (mag.max(axis=1) if x.shape[1] else np.zeros(x.shape[0], np.float32)) * (np.float32(1) / q_max)
     s = s.astype(np.float32)
     with np.errstate(all="ignore"):
         r = np.rint(x / s[:, None])

@@ -1,5 +1,5 @@
 // Activations to int8 codes with one scale for each row ("token"): the quantiser of Sec. III-A with the range taken from the row
-// itself.  s = max |x| / Q, q = clamp(rint(x / s), -Q, Q), every step in fp32; a row of zeros has s = 0 and codes 0.
+// itself.  s = max |x| * (1 / Q), q = clamp(rint(x / s), -Q, Q), every step in fp32; a row of zeros has s = 0 and codes 0.
 #pragma once
 #include "element.hpp"
 #include "elementwise.hpp"
@@ -11,7 +11,7 @@ constexpr int QT_THREADS = 256;
 // Codes of N elements of a row with scale s, inv = 1 / s.  rint(x / s) is decided by the product x inv, which is within 127 * 2^-22 < 4e-5 of the
 // quotient: adding 1.5 * 2^23 rounds it to an integer (half to even) in the low bits of the sum.  Where the product lies that close to a
 // half, or is NaN, the piece is done by IEEE division (`exact`: every piece, for scales whose reciprocal is no ordinary number).  An IEEE
-// division is 12 instructions an element, this is 5.  With s = max |x| / Q no quotient rounds beyond Q.
+// division is 12 instructions an element, this is 5.  With s within 2^-23 of max |x| / Q no quotient rounds beyond Q.
 template <int N>
 __device__ __forceinline__ void quantize_piece(const float (&x)[N], float s, float inv, float Q, bool exact, uint32_t (&codes)[N / 4]) {
     constexpr float MAGIC = 12582912.0f;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(QT_THREADS) void quantize_tokens_kernel(const typen
             for (int w = 1; w < WAVES; ++w) m = fmaxf(m, part[w]);
             __syncthreads();
         }
-        const float s = m / Q, inv = 1.0f / s;
+        const float s = m * (1.0f / Q), inv = 1.0f / s;
         const bool exact = !(s > 1.0e-30f && s < 1.0e30f);
         if (lane == 0) scales[r] = s;
 #pragma unroll
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(QT_THREADS) void quantize_long_tokens_kernel(const 
         __syncthreads();
         m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
         __syncthreads();
-        const float s = m / Q, inv = 1.0f / s;
+        const float s = m * (1.0f / Q), inv = 1.0f / s;
         const bool exact = !(s > 1.0e-30f && s < 1.0e30f);
         if (threadIdx.x == 0) scales[r] = s;
         for (size_t c = (size_t)threadIdx.x * P; c < whole; c += QT_THREADS * P) {

@@ -131,6 +131,14 @@ def test_quantize_tokens_at_odd_addresses(B, name, K):
     assert (q[3:].view(5, K).cpu().numpy() == ot.quantize_tokens(x, 8)[0]).all() and (q[:3] == 0).all()
 
 
+def test_quantize_tokens_codes_are_those_of_the_row_quantiser(B):
+    import torch
+    x = torch.randn((70, 513), generator=torch.Generator().manual_seed(3)).cuda()
+    for bits in (8, 5, 2):
+        q, s = B.adapt_quantize_tokens(x, bits)
+        assert torch.equal(q, B.adapt_quantize_rows_f32(x, s, bits))
+
+
 def test_quantize_tokens_without_columns(B):
     import torch
     s = torch.full((3,), 5.0, device="cuda")
