@@ -27,6 +27,7 @@ void launch_tile(adapt::TileParams p, const TilePlan &t, hipStream_t s) {
     p.tiles_i = (int)t.tiles_i;
     p.tiles_j = (int)t.tiles_j;
     p.Kb_split = (int)t.kb_split;
+    p.stream = (double)p.I * (double)p.J * sizeof(typename E::mem) > 32.0e6;
     adapt::tile_product_kernel<Op, E, TM, TN, SB, NB, DMA, TANH><<<dim3((unsigned)(t.tiles_i * t.tiles_j), (unsigned)t.split), adapt::TILE_THREADS, 0, s>>>(p);
 }
 
@@ -37,6 +38,7 @@ void launch_tiles(const adapt::TileParams &p, const TilePlan &t, hipStream_t s) 
         case TILE_256x256: launch_tile<Op, E, 256, 256, 64, 4, true>(p, t, s); break;
         case TILE_256x128: launch_tile<Op, E, 256, 128, 128, 3, true>(p, t, s); break;
         case TILE_128x128: launch_tile<Op, E, 128, 128, 128, 4, true>(p, t, s); break;
+        case TILE_128x128_TWO: launch_tile<Op, E, 128, 128, 64, 3, true>(p, t, s); break;
         case TILE_128x64: launch_tile<Op, E, 128, 64, 128, 4, true>(p, t, s); break;
         default: launch_tile<Op, E, 64, 64, 128, 4, true>(p, t, s); break;
     }
