@@ -552,7 +552,8 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
  *     db[n]    = sum_m dy[m][n]
  * dy_dev [M][N], dx_dev [M][K], dw_dev [N][K], db_dev [N] of element type `type`; codes and scales as in adapt_int8_linear.  Any of dx_dev,
  * dw_dev, db_dev may be NULL (not computed; a_dev and s_a_dev are read for dw alone, w_dev and s_w_dev for dx alone).  They are
- * fully overwritten.  M, K and N are at most 65535 * 64, M and N at most 2796160 (ADAPT_F32) (else ADAPT_ERR_UNSUPPORTED).  dy * s is formed in fp32 and kept to 24 bits (ADAPT_F32) or 16 bits (the 16-bit types, whose results keep 8 or 11).
+ * fully overwritten.  dy * s is formed in fp32 and kept to 24 bits (ADAPT_F32) or 16 bits (the 16-bit types, whose results keep 8 or 11).
+ * M, K and N are at most 2^21 and no matrix has 2^36 elements, else ADAPT_ERR_UNSUPPORTED.
  * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
  * dx_dev / dw_dev are given). */
 int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes);
@@ -568,7 +569,7 @@ int adapt_embedding(const void *table_dev, int type, const void *tokens_dev, int
 /* Its gradient: dtable[v] = scale * sum over the places t with tok[t] = v of dy[t]; rows of tokens that do not occur, and row
  * padding_idx (-1: none), are zero; places whose token is padding_idx or lies outside [0, V) take no part (their dy is not read).
  * dtable_dev [V][D] of dy's element type, fully overwritten.  The places are sorted by token, so no sum depends on an order of
- * atomics.  D <= 65535 * 64, else ADAPT_ERR_UNSUPPORTED.  workspace_dev: adapt_embedding_backward_workspace bytes. */
+ * atomics.  D <= 2^21, else ADAPT_ERR_UNSUPPORTED.  workspace_dev: adapt_embedding_backward_workspace bytes. */
 int adapt_embedding_backward_workspace(size_t tokens, int V, int D, size_t *bytes);
 int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_dev, int token_bits, void *dtable_dev, size_t tokens, int V, int D, float scale,
                              int64_t padding_idx, void *workspace_dev, size_t workspace_bytes, void *stream);

@@ -14,7 +14,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 constexpr int INT8_MAX_K = 131071;              // (-128)^2 K < 2^31
 constexpr long long MAX_TILES = 1ll << 24;      // a launch is limited to 2^32 threads
-constexpr int GRAD_MAX = 65535 * 64;            // a grid's second dimension
+constexpr int GRAD_MAX = 2097152;               // 256 rows of its pieces (6 bytes an element) are addressed with 32 bits
 
 int int8_args(const char *who, int M, int K, int N, int type) {
     if (M < 0 || K < 0 || N < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
@@ -126,7 +126,7 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
 // product.
 struct GradPlan {
     int Rp;                     // R in whole stages
-    long long row;              // bytes of a row: all pieces
+    long long row, row_b;       // bytes of a row of pieces, of codes
     TilePlan tile;
     size_t b, part, bytes;      // offsets (a at 0)
 };
@@ -134,9 +134,10 @@ GradPlan grad_plan(long long I, long long J, long long R, int P) {
     GradPlan g{};
     g.Rp = (int)((R + adapt::GRAD_STAGE - 1) / adapt::GRAD_STAGE * adapt::GRAD_STAGE);
     g.row = 2ll * P * g.Rp;
+    g.row_b = 2ll * g.Rp * (P == 3 ? adapt::code_copies<3> : adapt::code_copies<2>);
     g.tile = tile_plan(I, J, g.row, device_cus(), 8);
     g.b = round256((size_t)I * (size_t)g.row);
-    g.part = g.b + round256((size_t)J * (size_t)g.row);
+    g.part = g.b + round256((size_t)J * (size_t)g.row_b);
     g.bytes = g.part + (g.tile.split > 1 ? round256((size_t)g.tile.split * (size_t)I * (size_t)J * 4) : 0);
     return g;
 }
@@ -157,7 +158,9 @@ void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_
     p.I = I;
     p.J = J;
     p.Kb = (int)g.row;
-    p.lda = p.ldb = (uint32_t)g.row;
+    p.Kb_b = (int)g.row_b;
+    p.lda = (uint32_t)g.row;
+    p.ldb = (uint32_t)g.row_b;
     if (g.tile.split == 1) {
         p.c = c;
         launch_tiles<adapt::TileBF16, E>(p, g.tile, s);
@@ -229,8 +232,9 @@ int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want
     if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
     *bytes = 0;
     if (int rc = int8_args(who, M, K, N, type)) return rc;
-    if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
     const int P = grad_pieces(type);
+    if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
+    if ((long long)M * K >> 36 || (long long)N * K >> 36 || (long long)M * N >> 36) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a matrix of 2^36 elements or more", who);
     const size_t db = round256(db_blocks(M) * (size_t)N * 4);       // partial sums of the bias gradient: behind those of dw
     size_t need = db;
     if (want_dx && M && K) {
@@ -265,9 +269,6 @@ int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev
     if (int rc = adapt_int8_linear_backward_workspace(M, K, N, type, want_dx, want_dw, &need)) return rc;
     if (need && (!workspace_dev || workspace_bytes < need || off_by(workspace_dev, 256)))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, need);
-    const int P = grad_pieces(type);
-    // (a row of pieces is addressed with 32 bits, 256 rows of it with 32 unsigned)
-    if (2ll * P * (((M > N ? M : N) + 63ll) / 64 * 64) * 256 > 0xffffffffll) return fail(ADAPT_ERR_UNSUPPORTED, "%s: M or N too large", who);
     const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, nullptr, nullptr, M, K, N, 0};
     char *const ws = static_cast<char *>(workspace_dev);
     void *const dx = want_dx ? dx_dev : nullptr, *const dw = want_dw ? dw_dev : nullptr, *const db = want_db ? db_dev : nullptr;

@@ -61,6 +61,8 @@ EmbedPlan embed_plan(size_t T, int V, int D) {
     return e;
 }
 
+constexpr int EMBED_MAX_D = 1 << 21;            // the runs' launch stays below 2^32 threads
+
 int embed_args(const char *who, size_t T, int V, int D) {
     if (V < 0 || D < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
     if (T >= (1ull << 31)) return fail(ADAPT_ERR_UNSUPPORTED, "%s: more than 2^31-1 tokens", who);
@@ -186,6 +188,7 @@ int adapt_embedding_backward_workspace(size_t tokens, int V, int D, size_t *byte
     if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
     *bytes = 0;
     if (int rc = embed_args(who, tokens, V, D)) return rc;
+    if (D > EMBED_MAX_D) return fail(ADAPT_ERR_UNSUPPORTED, "%s: rows of more than %d elements", who, EMBED_MAX_D);
     *bytes = embed_plan(tokens, V, D).bytes;
     return ADAPT_OK;
 }
@@ -197,7 +200,7 @@ int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_de
     if (!e) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: element type %d is none of ADAPT_F32, ADAPT_F16, ADAPT_BF16", who, type);
     if (token_bits != 32 && token_bits != 64) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: token_bits=%d is neither 32 nor 64", who, token_bits);
     if (int rc = embed_args(who, tokens, V, D)) return rc;
-    if (D > 65535 * 64) return fail(ADAPT_ERR_UNSUPPORTED, "%s: rows of more than %d elements", who, 65535 * 64);
+    if (D > EMBED_MAX_D) return fail(ADAPT_ERR_UNSUPPORTED, "%s: rows of more than %d elements", who, EMBED_MAX_D);
     if (!V || !D) return ADAPT_OK;
     if (!dtable_dev || (tokens && (!tokens_dev || !dy_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
     if (off_by(dy_dev, e) || off_by(dtable_dev, e) || off_by(tokens_dev, (size_t)token_bits / 8))

@@ -3,16 +3,21 @@
 //     dx[m][k] = sum_n (dy[m][n] s_w[n]) w[n][k],      dw[n][k] = sum_m (dy[m][n] s_a[m]) a[m][k]
 //
 // Codes are bf16 numbers.  dy s is a sum of bf16 numbers, t = t0 + t1 (+ t2), each the rest of the one before it rounded to nearest: 16
-// (24) bits.  So a gradient is one bf16 product with exact partial products and fp32 sums, over rows [t2 2^16 | t1 2^8 | t0] and
-// [q 2^-16 | q 2^-8 | q]: the powers of two keep the small pieces of small gradients above the smallest number (unscaled, gradients below
-// 2^-110 would lose bits), and the small pieces come first.  Both matrices are written to the workspace with the summed index last,
-// rows in whole stages of 128 bytes.
+// (24) bits.  So a gradient is one bf16 product with exact partial products and fp32 sums, over rows [t1 | t0] that meet the same codes q twice,
+// or, where 24 bits are kept, rows [t2 2^16 | t1 2^8 | t0] and [q 2^-16 | q 2^-8 | q]: the powers of two keep the small pieces of small
+// gradients above the smallest number (unscaled, fp32 gradients below 2^-110 would lose bits; of a 16-bit type only those below 2^-117 that its results
+// do not show).  The small pieces come first.  The matrices are written to the workspace with the summed index last, rows in whole
+// stages of 128 bytes.
 #pragma once
 #include "tile_product.hpp"
 
 namespace adapt {
 
 constexpr int GRAD_STAGE = 64;      // elements of a row that a product takes at a time: pieces are padded to a multiple of them
+
+// numbers a code is written as, P pieces to be met
+template <int P>
+constexpr int code_copies = P == 3 ? 3 : 1;
 
 // piece z = 0 (the smallest) .. P - 1 of t
 template <int P>
@@ -21,7 +26,7 @@ __device__ __forceinline__ void split_pieces(float t, __bf16 (&out)[P]) {
     const bool finite = fabsf((float)out[P - 1]) < __builtin_inff();        // (infinities and NaN: the first piece alone)
 #pragma unroll
     for (int z = P - 2; z >= 0; --z) {
-        t = (t - (float)out[z + 1]) * 256.0f;               // exact: the rest has no more bits than t
+        t = (t - (float)out[z + 1]) * (P == 3 ? 256.0f : 1.0f);        // exact: the rest has no more bits than t
         if (!finite) t = 0.0f;
         out[z] = (__bf16)t;
     }
@@ -150,9 +155,10 @@ __global__ __launch_bounds__(1024) void grad_bias_kernel(const float *__restrict
     }
 }
 
-// out[c][z][r] = q[r][c] * 2^(-8 (P - 1 - z))
+// out[c][z][r] = q[r][c] * 2^(-8 (copies - 1 - z))
 template <int P>
 __global__ __launch_bounds__(256) void grad_codes_kernel(const int8_t *__restrict__ q, __bf16 *__restrict__ out, int R, int C, int Rp) {
+    constexpr int Z = code_copies<P>;
     __shared__ float tile[64][GRAD_LD];
     const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
     const int rl = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16, r = r0 + rl;
@@ -172,12 +178,12 @@ __global__ __launch_bounds__(256) void grad_codes_kernel(const int8_t *__restric
     __syncthreads();
     grad_transposed(tile, C, [&](int col, int row, const float(&t)[8]) {
 #pragma unroll
-        for (int z = 0; z < P; ++z) {
-            const float f = z == P - 1 ? 1.0f : (z == P - 2 ? 0x1p-8f : 0x1p-16f);
+        for (int z = 0; z < Z; ++z) {
+            const float f = z == Z - 1 ? 1.0f : (z == Z - 2 ? 0x1p-8f : 0x1p-16f);
             bf16x8_t b;
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] = (__bf16)(t[j] * f);
-            *reinterpret_cast<bf16x8_t *>(out + ((size_t)col * P + z) * (size_t)Rp + row) = b;
+            *reinterpret_cast<bf16x8_t *>(out + ((size_t)col * Z + z) * (size_t)Rp + row) = b;
         }
     });
 }

@@ -19,6 +19,7 @@ constexpr int TILE_THREADS = 256;       // four waves, 2 x 2 over the tile
 struct TileParams {
     const char *a, *b;
     int I, J, Kb;               // Kb: bytes of a row that are summed over
+    int Kb_b;                   // bf16: bytes of a row of b (whole stages), which meets a's again and again
     uint32_t lda, ldb;          // bytes from row to row
     int tiles_i, tiles_j;
     // int8: rescaling by row and column, bias, activation
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
     // requests: number q of a wave covers rows 8 (4 q + wave) .. + 7 of the tile, lane l row l / 8, piece (l % 8) ^ (row % 8)
     auto swizzle = [](int row) { return SB == 256 ? row & 15 : SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
     const int prow = lane / PIECES, piece16 = ((lane % PIECES) ^ swizzle(RQ * wave + prow)) * 16;
-    const char *abase = p.a + (size_t)i0 * p.lda + k0, *bbase = p.b + (size_t)j0 * p.ldb + k0;
+    const char *abase = p.a + (size_t)i0 * p.lda + k0, *bbase = p.b + (size_t)j0 * p.ldb;
     uint32_t voff[NQ];
 #pragma unroll
     for (int q = 0; q < QA; ++q) voff[q] = (uint32_t)min(RQ * (4 * q + wave) + prow, p.I - 1 - i0) * p.lda + (DMA ? (uint32_t)piece16 : 0u);
@@ -151,7 +152,8 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
 
     if constexpr (DMA) {
         int dma_s = 0;          // stage that is requested next
-        const char *da = abase, *db = bbase;
+        int kb = Op::INT ? 0 : k0 % p.Kb_b;
+        const char *da = abase, *db = bbase + kb;
         auto dma_begin = [&]() {        // where the last stage is not whole, lanes whose piece lies behind the end fetch its first piece instead
             if (Op::INT && dma_s == full && piece16 >= rest)
 #pragma unroll
@@ -165,6 +167,13 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
             da += SB;
             db += SB;
             ++dma_s;
+            if constexpr (!Op::INT) {
+                kb += SB;
+                if (kb == p.Kb_b) {
+                    kb = 0;
+                    db = bbase;
+                }
+            }
         };
         auto dma_stage = [&](int buf) {
             dma_begin();

@@ -545,6 +545,77 @@ def test_a_stream_given_to_the_call(B):
     assert all(torch.equal(g, want) for g in got) and noise[0][0] == 3.0
 
 
+# ---------------------------------------------------------------------------------------------- beyond 32 bits of offset
+
+@pytest.fixture
+def big():
+    """Tensors of 8 to 20 GB: nothing of them stays."""
+    import torch
+    torch.cuda.empty_cache()
+    yield torch
+    torch.cuda.empty_cache()
+
+
+def test_quantize_tokens_beyond_32_bits(B, big):
+    torch = big
+    x = torch.empty((280000, 16384), dtype=torch.bfloat16, device="cuda")        # 4.6e9 elements
+    x[-3:] = torch.randn((3, 16384), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    x[:-3].fill_(1)
+    q, s = B.adapt_quantize_tokens(x, 8)
+    wq, ws = ot.quantize_tokens(x[-3:].float().cpu().numpy(), 8)
+    assert (q[-3:].cpu().numpy() == wq).all() and (s[-3:].cpu().numpy() == ws).all()
+    assert (q[0] == 127).all() and (q[-4] == 127).all()
+
+
+@pytest.mark.parametrize("K", [16, 17])
+def test_int8_linear_beyond_32_bits(B, big, K):
+    torch = big
+    rng = np.random.default_rng(K)
+    M, N = 140000, 33000                                                        # 4.6e9 results
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    y = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), dtype=torch.bfloat16)
+    for rows in (slice(0, 2), slice(65070, 65080), slice(M - 5, M)):
+        same_bits(y[rows], rounded(ot.int8_linear(a[rows], s_a[rows], w, s_w), "bf16"))
+
+
+def test_int8_linear_backward_beyond_32_bits(B, big):
+    torch = big
+    rng = np.random.default_rng(5)
+    M, K, N = 1 << 20, 4200, 5                                                  # dx of 4.4e9 elements
+    w, s_w = codes(rng, N, K), scales(rng, N)
+    dy, dyd = randn(rng, (M, N), "bf16")
+    a = torch.zeros((M, K), dtype=torch.int8, device="cuda")
+    dx, _, _ = B.adapt_int8_linear_backward(dyd, a, torch.ones(M, device="cuda"), dev(w), dev(s_w), want=("dx",))
+    for rows in (slice(0, 3), slice(1022600, 1022610), slice(M - 3, M)):
+        (want, mass), _, _ = ot.int8_linear_backward(dy[rows], np.zeros((dy[rows].shape[0], K), np.int8), np.ones(dy[rows].shape[0], np.float32), w, s_w)
+        within(dx[rows], want, mass, N, "bf16", 2.0 ** -17)
+
+
+def test_embedding_beyond_32_bits(B, big):
+    torch = big
+    V, D = 70000, 65536                                                         # 4.6e9 elements
+    table = torch.empty((V, D), dtype=torch.float16, device="cuda")
+    rows = [V - 1, 3, V - 2, 65540]
+    table[rows] = torch.randn((4, D), generator=torch.Generator().manual_seed(2)).half().cuda()
+    got = B.adapt_embedding(table, torch.tensor(rows, device="cuda"), scale=0.5)
+    same_bits(got, (table[rows].float().cpu() * 0.5).half())
+    tok = torch.tensor([V - 1, 65540, V - 1, 2], device="cuda")
+    B.adapt_embedding_backward(got, tok, V, out=table)
+    want, mass, n = ot.embedding_backward(got.float().cpu().numpy(), np.array([2, 1, 2, 0]), 3, 1.0)
+    within(table[[2, 65540, V - 1]], want, mass, n[:, None], "f16")
+    assert (table[3:65540:6007] == 0).all() and (table[-2] == 0).all() and (table[-3:-1] == 0).all()
+
+
+def test_dropout_beyond_32_bits(B, big):
+    torch = big
+    n = (1 << 32) + 1011
+    x = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    B.adapt_dropout(x, 0.5, 17, 3, out=x)
+    for first in (0, (1 << 32) - 500, n - 1000):
+        kept = ot.dropout_kept(1000, 0.5, 17, 3, first=first)
+        assert (f64(x[first:first + 1000]) == np.where(kept, 2.0, 0.0)).all()
+
+
 def test_binding_refuses_what_it_cannot_pass_on(B):
     import torch
     a = torch.zeros((4, 8), dtype=torch.int8, device="cuda")

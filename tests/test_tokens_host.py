@@ -61,6 +61,8 @@ def test_int8_linear_backward_refusals(lib):
     assert lib.adapt_int8_linear_backward_workspace(4, 4, 4, 0, 1, 1, None) == -1
     assert lib.adapt_int8_linear_backward_workspace(-4, 4, 4, 0, 1, 1, ctypes.byref(n)) == -1 and n.value == 0
     assert lib.adapt_int8_linear_backward_workspace(4, 4, 4, 5, 1, 1, ctypes.byref(n)) == -1
+    for sizes in (((1 << 21) + 1, 4, 4), (4, (1 << 21) + 1, 4), (4, 4, (1 << 21) + 1), (1 << 20, 1 << 16, 4), (4, 1 << 16, 1 << 20), (1 << 20, 4, 1 << 16)):
+        assert lib.adapt_int8_linear_backward_workspace(*sizes, 0, 1, 1, ctypes.byref(n)) == -2 and n.value == 0
     assert lib.adapt_int8_linear_backward_workspace(64, 48, 32, 0, 1, 1, ctypes.byref(n)) == 0
     need = n.value
     good = dict(dy=vp(256), type=0, a=vp(512), s_a=vp(768), w=vp(1024), s_w=vp(1280), M=64, K=48, N=32, dx=vp(2048), dw=vp(4096), db=vp(8192),
@@ -99,6 +101,7 @@ def test_embedding_refusals(lib):
     assert lib.adapt_embedding_backward_workspace(4, 8, 16, None) == -1
     assert lib.adapt_embedding_backward_workspace(4, -8, 16, ctypes.byref(n)) == -1 and n.value == 0
     assert lib.adapt_embedding_backward_workspace(1 << 31, 8, 16, ctypes.byref(n)) == -2
+    assert lib.adapt_embedding_backward_workspace(4, 8, (1 << 21) + 1, ctypes.byref(n)) == -2 and n.value == 0
     assert lib.adapt_embedding_backward_workspace(4, 8, 16, ctypes.byref(n)) == 0
     need = n.value
     assert need > 0
@@ -112,7 +115,7 @@ def test_embedding_refusals(lib):
     assert bad(dy=vp(258)) == -1 and bad(tok=vp(516)) == -1 and bad(out=vp(1026)) == -1 and bad(ws=vp(4097)) == -1
     assert bad(n=need - 1) == -1 and "workspace" in _text(lib)
     assert bad(out=vp(256)) == -1 and "alias" in _text(lib)
-    assert bad(T=1 << 31) == -2
+    assert bad(T=1 << 31) == -2 and bad(D=(1 << 21) + 1) == -2
     assert bad(V=0, out=None) == 0 and bad(D=0, out=None) == 0
 
 
