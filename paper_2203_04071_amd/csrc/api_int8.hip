@@ -122,39 +122,38 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
     else launch_tile<adapt::TileI8, E, 64, 64, 64, 2, false>(p, small, s);
 }
 
-// Workspace of one gradient c [I][J], the sums over R: rows of the pieces of dy s [I], rows of codes [J], partial sums of a split
-// product.
+// Workspace of one gradient c [I][J], the sums over R: rows of the pieces of dy s [I], rows of codes [J], the rows' exponents, partial sums of
+// a split product.
 struct GradPlan {
     int Rp;                     // R in whole stages
     long long row, row_b;       // bytes of a row of pieces, of codes
     TilePlan tile;
-    size_t b, part, bytes;      // offsets (a at 0)
+    size_t b, exps, part, bytes;    // offsets (a at 0)
 };
 GradPlan grad_plan(long long I, long long J, long long R, int P) {
     GradPlan g{};
     g.Rp = (int)((R + adapt::GRAD_STAGE - 1) / adapt::GRAD_STAGE * adapt::GRAD_STAGE);
     g.row = 2ll * P * g.Rp;
-    g.row_b = 2ll * g.Rp * (P == 3 ? adapt::code_copies<3> : adapt::code_copies<2>);
+    g.row_b = 2ll * g.Rp;
     g.tile = tile_plan(I, J, g.row, device_cus(), 8);
     g.b = round256((size_t)I * (size_t)g.row);
-    g.part = g.b + round256((size_t)J * (size_t)g.row_b);
+    g.exps = g.b + round256((size_t)J * (size_t)g.row_b);
+    g.part = g.exps + round256((size_t)I * 4);
     g.bytes = g.part + (g.tile.split > 1 ? round256((size_t)g.tile.split * (size_t)I * (size_t)J * 4) : 0);
     return g;
 }
-int grad_pieces(int type) { return type == ADAPT_F32 ? 3 : 2; }
+int grad_pieces(int type) { return type == ADAPT_BF16 ? 1 : 2; }
 
-size_t db_blocks(int M) { return ((size_t)M + 63) / 64; }        // rows of partial sums of the bias gradient
-
-template <class E>
-void join(const float *part, int parts, size_t n, void *c, hipStream_t s) {
-    adapt::grad_join_kernel<E><<<ew_grid(n / 4 + 1), 256, 0, s>>>(part, parts, n, static_cast<typename E::mem *>(c));
-}
+// rows of partial results of the columns: sums, largest elements
+size_t column_blocks(int M) { return ((size_t)M + adapt::GRAD_ROWS - 1) / adapt::GRAD_ROWS; }
+size_t column_bytes(int M, int N) { return 2 * round256((M ? column_blocks(M) : 1) * (size_t)N * 4); }
 
 template <class E>
 void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_t s) {
     adapt::TileParams p{};
     p.a = ws;
     p.b = ws + g.b;
+    p.exp_i = reinterpret_cast<const int *>(ws + g.exps);
     p.I = I;
     p.J = J;
     p.Kb = (int)g.row;
@@ -163,44 +162,58 @@ void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_
     p.ldb = (uint32_t)g.row_b;
     if (g.tile.split == 1) {
         p.c = c;
-        launch_tiles<adapt::TileBF16, E>(p, g.tile, s);
+        launch_tiles<adapt::TileF16, E>(p, g.tile, s);
     } else {
-        p.c = ws + g.part;
-        launch_tiles<adapt::TileBF16, adapt::F32>(p, g.tile, s);
-        join<E>(reinterpret_cast<const float *>(ws + g.part), g.tile.split, (size_t)I * (size_t)J, c, s);
+        float *const part = reinterpret_cast<float *>(ws + g.part);
+        const size_t n = (size_t)I * (size_t)J;
+        p.c = part;
+        launch_tiles<adapt::TileF16, adapt::F32>(p, g.tile, s);
+        adapt::grad_join_kernel<E><<<ew_grid(n / 4 + 1), 256, 0, s>>>(part, g.tile.split, n, static_cast<typename E::mem *>(c));
     }
 }
 
 dim3 blocks64(int R, int C) { return dim3((unsigned)((R + 63) / 64), (unsigned)((C + 63) / 64)); }
 
+// a wave per row up to 2048 elements, a workgroup up to 8192 (quantize_tokens has the same rule); a workgroup takes several rows, whose scales
+// of the columns it reads once
+template <class E, int P>
+void grad_rows(const typename E::mem *dy, const float *s_w, _Float16 *a, int *exps, int M, int N, int Np, hipStream_t s) {
+    constexpr int T = adapt::GRAD_THREADS;
+    const unsigned by_wave = (unsigned)((M + 3) / 4 < 2048 ? (M + 3) / 4 : 2048), by_group = (unsigned)(M < 2048 ? M : 2048);
+    if (Np <= 512) adapt::grad_rows_kernel<E, P, 64, 1><<<by_wave, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+    else if (Np <= 1024) adapt::grad_rows_kernel<E, P, 64, 2><<<by_wave, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+    else if (Np <= 2048) adapt::grad_rows_kernel<E, P, T, 1><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+    else if (Np <= 4096) adapt::grad_rows_kernel<E, P, T, 2><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+    else if (Np <= 8192) adapt::grad_rows_kernel<E, P, T, 4><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+    else adapt::grad_long_rows_kernel<E, P><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+}
+
 template <class E, int P>
 void gradients(const adapt::Int8Params &q, const void *dy_dev, void *dx, void *dw, void *db, char *ws, hipStream_t s) {
-    const typename E::mem *const dy = static_cast<const typename E::mem *>(dy_dev);
-    __bf16 *const a = reinterpret_cast<__bf16 *>(ws);
+    typedef typename E::mem mem;
+    const mem *const dy = static_cast<const mem *>(dy_dev);
+    _Float16 *const a = reinterpret_cast<_Float16 *>(ws);
     if (dx) {
         const GradPlan g = grad_plan(q.M, q.K, q.N, P);
-        __bf16 *const b = reinterpret_cast<__bf16 *>(ws + g.b);
-        if (g.Rp) {
-            adapt::grad_split_rows_kernel<E, P><<<ew_grid((size_t)q.M * g.Rp / 8), 256, 0, s>>>(dy, q.s_w, a, q.M, q.N, g.Rp);
-            adapt::grad_codes_kernel<P><<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.w, b, q.N, q.K, g.Rp);
-        }
+        grad_rows<E, P>(dy, q.s_w, a, reinterpret_cast<int *>(ws + g.exps), q.M, q.N, g.Rp, s);
+        if (g.Rp) adapt::grad_codes_kernel<<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.w, reinterpret_cast<_Float16 *>(ws + g.b), q.N, q.K, g.Rp);
         grad_product<E>(g, ws, q.M, q.K, dx, s);
     }
-    const size_t blocks = db_blocks(q.M);
-    if (dw) {
-        const GradPlan g = grad_plan(q.N, q.K, q.M, P);
-        __bf16 *const b = reinterpret_cast<__bf16 *>(ws + g.b);
-        float *const part = db ? reinterpret_cast<float *>(ws + g.bytes) : nullptr;
-        if (g.Rp) {
-            adapt::grad_split_columns_kernel<E, P, true><<<blocks64(g.Rp, q.N), 256, 0, s>>>(dy, q.s_a, a, part, q.M, q.N, g.Rp);
-            adapt::grad_codes_kernel<P><<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.a, b, q.M, q.K, g.Rp);
+    if (dw || db) {
+        const GradPlan g = dw ? grad_plan(q.N, q.K, q.M, P) : GradPlan{};
+        const int blocks = (int)column_blocks(q.M);
+        float *const sum = db ? reinterpret_cast<float *>(ws + g.bytes) : nullptr;
+        float *const big = dw ? reinterpret_cast<float *>(ws + g.bytes + column_bytes(q.M, q.N) / 2) : nullptr;
+        int *const exps = reinterpret_cast<int *>(ws + g.exps);
+        if (blocks) adapt::grad_columns_kernel<E><<<dim3((unsigned)blocks, (unsigned)((q.N + 63) / 64)), 256, 0, s>>>(dy, q.s_a, sum, big, q.M, q.N);
+        adapt::grad_columns_join_kernel<E><<<(unsigned)((q.N + 63) / 64), 1024, 0, s>>>(sum, big, static_cast<mem *>(db), exps, blocks, q.N);
+        if (dw) {
+            if (g.Rp) {
+                adapt::grad_turned_rows_kernel<E, P><<<blocks64(g.Rp, q.N), 256, 0, s>>>(dy, q.s_a, exps, a, q.M, q.N, g.Rp);
+                adapt::grad_codes_kernel<<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.a, reinterpret_cast<_Float16 *>(ws + g.b), q.M, q.K, g.Rp);
+            }
+            grad_product<E>(g, ws, q.N, q.K, dw, s);
         }
-        if (db) adapt::grad_bias_kernel<E><<<(unsigned)((q.N + 63) / 64), 1024, 0, s>>>(part, static_cast<typename E::mem *>(db), (int)blocks, q.N);
-        grad_product<E>(g, ws, q.N, q.K, dw, s);
-    } else if (db) {
-        float *const part = reinterpret_cast<float *>(ws);
-        if (blocks) adapt::grad_split_columns_kernel<E, P, false><<<blocks64(q.M, q.N), 256, 0, s>>>(dy, nullptr, nullptr, part, q.M, q.N, 0);
-        adapt::grad_bias_kernel<E><<<(unsigned)((q.N + 63) / 64), 1024, 0, s>>>(part, static_cast<typename E::mem *>(db), (int)blocks, q.N);
     }
 }
 
@@ -235,14 +248,10 @@ int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want
     const int P = grad_pieces(type);
     if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
     if ((long long)M * K >> 36 || (long long)N * K >> 36 || (long long)M * N >> 36) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a matrix of 2^36 elements or more", who);
-    const size_t db = round256(db_blocks(M) * (size_t)N * 4);       // partial sums of the bias gradient: behind those of dw
-    size_t need = db;
+    size_t need = column_bytes(M, N);       // partial results of the columns: behind what dw needs
+    if (want_dw && N && K) need += grad_plan(N, K, M, P).bytes;
     if (want_dx && M && K) {
         const size_t b = grad_plan(M, K, N, P).bytes;
-        need = b > need ? b : need;
-    }
-    if (want_dw && N && K) {
-        const size_t b = grad_plan(N, K, M, P).bytes + db;
         need = b > need ? b : need;
     }
     *bytes = need;
@@ -273,9 +282,9 @@ int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev
     char *const ws = static_cast<char *>(workspace_dev);
     void *const dx = want_dx ? dx_dev : nullptr, *const dw = want_dw ? dw_dev : nullptr, *const db = want_db ? db_dev : nullptr;
     hipStream_t s = (hipStream_t)stream;
-    if (type == ADAPT_F32) gradients<adapt::F32, 3>(p, dy_dev, dx, dw, db, ws, s);
+    if (type == ADAPT_F32) gradients<adapt::F32, 2>(p, dy_dev, dx, dw, db, ws, s);
     else if (type == ADAPT_F16) gradients<adapt::F16, 2>(p, dy_dev, dx, dw, db, ws, s);
-    else gradients<adapt::BF16, 2>(p, dy_dev, dx, dw, db, ws, s);
+    else gradients<adapt::BF16, 1>(p, dy_dev, dx, dw, db, ws, s);
     HIP_TRY(hipGetLastError());
     return ADAPT_OK;
 }

@@ -2,69 +2,222 @@
 //
 //     dx[m][k] = sum_n (dy[m][n] s_w[n]) w[n][k],      dw[n][k] = sum_m (dy[m][n] s_a[m]) a[m][k]
 //
-// Codes are bf16 numbers.  dy s is a sum of bf16 numbers, t = t0 + t1 (+ t2), each the rest of the one before it rounded to nearest: 16
-// (24) bits.  So a gradient is one bf16 product with exact partial products and fp32 sums, over rows [t1 | t0] that meet the same codes q twice,
-// or, where 24 bits are kept, rows [t2 2^16 | t1 2^8 | t0] and [q 2^-16 | q 2^-8 | q]: the powers of two keep the small pieces of small
-// gradients above the smallest number (unscaled, fp32 gradients below 2^-110 would lose bits; of a 16-bit type only those below 2^-117 that its results
-// do not show).  The small pieces come first.  The matrices are written to the workspace with the summed index last, rows in whole
-// stages of 128 bytes.
+// Both are c[i][j] = sum_r t[i][r] q[j][r] with codes q, which are fp16 numbers.  t = dy s becomes fp16 numbers as well: every row i is brought to
+// a largest element in [2^14, 2^15) by a power of two, which goes back in on the sums, and is then one fp16 number (11 bits: bf16 gradients, whose
+// results keep 8; a term is off by 2^-11 of itself at most, independently of the others, where the result is rounded by 2^-8) or the sum of
+// two, t = t0 + t1, t1 the rest that t0 leaves (22 bits: fp16 and fp32 gradients; 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at
+// every addition).  Elements below 2^-18 (22 bits) or 2^-29 (11 bits) of their row's largest keep fewer bits; what they lose is below 2^-40 of that largest.  So a
+// gradient is an fp16 product with exact partial products and fp32 sums over rows [t1 | t0] that meet the same codes twice, the small pieces first.
+// (Three bf16 pieces of 24 bits, without the rows' powers of two, took 148 us where this takes SEQ for 6400 x 512 -> 2048 fp32; two of them 470 us
+// against BIG for 4096^3 bf16.)
+//
+// Both matrices are written to the workspace with the summed index last, rows in whole stages of 128 bytes.
 #pragma once
 #include "tile_product.hpp"
 
 namespace adapt {
 
 constexpr int GRAD_STAGE = 64;      // elements of a row that a product takes at a time: pieces are padded to a multiple of them
+constexpr int GRAD_THREADS = 256;
 
-// numbers a code is written as, P pieces to be met
-template <int P>
-constexpr int code_copies = P == 3 ? 3 : 1;
+// exponent e of a row with largest element m: m 2^-e lies in [2^14, 2^15)
+__device__ __forceinline__ int grad_exponent(float m) {
+    if (!(m > 0.0f)) return 0;
+    return (m < __builtin_inff() ? __builtin_amdgcn_frexp_expf(m) : 128) - 15;
+}
 
-// piece z = 0 (the smallest) .. P - 1 of t
+// piece z = 0 (the smaller) .. P - 1 of t 2^-e
 template <int P>
-__device__ __forceinline__ void split_pieces(float t, __bf16 (&out)[P]) {
-    out[P - 1] = (__bf16)t;
-    const bool finite = fabsf((float)out[P - 1]) < __builtin_inff();        // (infinities and NaN: the first piece alone)
+__device__ __forceinline__ void split_pieces(float t, int e, _Float16 (&out)[P]) {
+    t = __builtin_amdgcn_ldexpf(t, -e);
+    out[P - 1] = (_Float16)t;
+    if constexpr (P == 2) {
+        const float hi = (float)out[1];
+        out[0] = fabsf(hi) < __builtin_inff() ? (_Float16)(t - hi) : (_Float16)0.0f;        // (t - hi is exact; infinities and NaN: the first piece alone)
+    }
+}
+template <int P>
+__device__ __forceinline__ void store_pieces(const float (&t)[8], int e, _Float16 *out, size_t next) {      // next: elements to the piece behind
+    f16x8_t v[P];
 #pragma unroll
-    for (int z = P - 2; z >= 0; --z) {
-        t = (t - (float)out[z + 1]) * (P == 3 ? 256.0f : 1.0f);        // exact: the rest has no more bits than t
-        if (!finite) t = 0.0f;
-        out[z] = (__bf16)t;
+    for (int j = 0; j < 8; ++j) {
+        _Float16 q[P];
+        split_pieces<P>(t[j], e, q);
+#pragma unroll
+        for (int z = 0; z < P; ++z) v[z][j] = q[z];
+    }
+#pragma unroll
+    for (int z = 0; z < P; ++z) *reinterpret_cast<f16x8_t *>(out + z * next) = v[z];
+}
+
+// eight elements n .. n + 7 of a row of N, zeros beyond its end
+template <typename E>
+__device__ __forceinline__ void load_eight(const typename E::mem *__restrict__ row, int n, int N, float (&t)[8]) {
+    if (n + 8 <= N) {
+        load_piece<E, 8>(row + n, t);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = n + j < N ? E::load(row[n + j]) : 0.0f;
     }
 }
 
-// out[m][z][n] = piece z of dy[m][n] * s[n], zeros for N <= n < Np; eight elements per thread
+// out[m][z][n] = piece z of dy[m][n] * s[n], exps[m]; zeros for N <= n < Np.  GROUP lanes share a row, NP times eight elements each, which stay in
+// registers between the maximum and the pieces; a lane's columns are the same in every row, their scales are read once.
+template <typename E, int P, int GROUP, int NP>
+__global__ __launch_bounds__(GRAD_THREADS) void grad_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out,
+                                                                 int *__restrict__ exps, int M, int N, int Np) {
+    constexpr int WAVES = GROUP / 64;
+    __shared__ float part[GRAD_THREADS / 64];
+    const int lane = threadIdx.x % GROUP, stride = (int)gridDim.x * (GRAD_THREADS / GROUP);
+    float sc[NP][8];
+#pragma unroll
+    for (int u = 0; u < NP; ++u) load_eight<F32>(s, (u * GROUP + lane) * 8, N, sc[u]);
+    for (int m = (int)blockIdx.x * (GRAD_THREADS / GROUP) + (int)threadIdx.x / GROUP; m < M; m += stride) {
+        float t[NP][8], big = 0.0f;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) load_eight<E>(dy + (size_t)m * (size_t)N, (u * GROUP + lane) * 8, N, t[u]);
+#pragma unroll
+        for (int u = 0; u < NP; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                t[u][j] = (u * GROUP + lane) * 8 + j < N ? t[u][j] * sc[u][j] : 0.0f;
+                big = fmaxf(big, fabsf(t[u][j]));
+            }
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) big = fmaxf(big, __shfl_xor(big, off, 64));
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = big;
+            __syncthreads();
+            big = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+            __syncthreads();
+        }
+        const int e = grad_exponent(big);
+        if (lane == 0) exps[m] = e;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+            const int n = (u * GROUP + lane) * 8;
+            if (n < Np) store_pieces<P>(t[u], e, out + (size_t)m * P * (size_t)Np + n, (size_t)Np);
+        }
+    }
+}
+
+// The same for rows too long for registers: read twice.
 template <typename E, int P>
-__global__ __launch_bounds__(256) void grad_split_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, __bf16 *__restrict__ out, int M,
-                                                              int N, int Np) {
-    const int per_row = Np / 8;
-    const size_t total = (size_t)M * per_row, stride = (size_t)gridDim.x * 256;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
-        const size_t m = i / per_row;
-        const int n = (int)(i - m * per_row) * 8;
-        float t[8];
-        const typename E::mem *const row = dy + m * (size_t)N;
-        if (n + 8 <= N) {
-            load_piece<E, 8>(row + n, t);
+__global__ __launch_bounds__(GRAD_THREADS) void grad_long_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out,
+                                                                      int *__restrict__ exps, int M, int N, int Np) {
+    __shared__ float part[GRAD_THREADS / 64];
+    for (int m = blockIdx.x; m < M; m += gridDim.x) {
+        float big = 0.0f;
+        auto eight = [&](int n, float(&t)[8]) {
+            float sc[8];
+            load_eight<E>(dy + (size_t)m * (size_t)N, n, N, t);
+            load_eight<F32>(s, n, N, sc);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] *= s[n + j];
-        } else {
+            for (int j = 0; j < 8; ++j) t[j] = n + j < N ? t[j] * sc[j] : 0.0f;
+        };
+        for (int n = threadIdx.x * 8; n < N; n += GRAD_THREADS * 8) {
+            float t[8];
+            eight(n, t);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = n + j < N ? E::load(row[n + j]) * s[n + j] : 0.0f;
-        }
-        bf16x8_t v[P];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            __bf16 q[P];
-            split_pieces<P>(t[j], q);
-#pragma unroll
-            for (int z = 0; z < P; ++z) v[z][j] = q[z];
+            for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(t[j]));
         }
 #pragma unroll
-        for (int z = 0; z < P; ++z) *reinterpret_cast<bf16x8_t *>(out + (m * P + z) * (size_t)Np + n) = v[z];
+        for (int off = 32; off > 0; off >>= 1) big = fmaxf(big, __shfl_xor(big, off, 64));
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = big;
+        __syncthreads();
+        big = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        __syncthreads();
+        const int e = grad_exponent(big);
+        if (threadIdx.x == 0) exps[m] = e;
+        for (int n = threadIdx.x * 8; n < Np; n += GRAD_THREADS * 8) {
+            float t[8];
+            eight(n, t);
+            store_pieces<P>(t, e, out + (size_t)m * P * (size_t)Np + n, (size_t)Np);
+        }
     }
 }
 
-// 64 x 64 elements src[r][c] come out as out[c][z][r], padded with zeros to Rp rows: the transposed operands.  A workgroup holds the block in
+// Of every column n over GRAD_ROWS rows: sum[block][n] of dy (sum != nullptr), big[block][n] = max |dy s| (big != nullptr).  Sixteen threads per
+// four columns, every sixteenth row each.
+constexpr int GRAD_ROWS = 256;
+template <typename E>
+__global__ __launch_bounds__(GRAD_THREADS) void grad_columns_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, float *__restrict__ sum,
+                                                                    float *__restrict__ big, int M, int N) {
+    __shared__ float sums[16][64], bigs[16][64];
+    const int c = (threadIdx.x & 15) * 4, n = blockIdx.y * 64 + c, g = threadIdx.x >> 4;
+    float a[4] = {}, b[4] = {};
+#pragma unroll
+    for (int u0 = 0; u0 < GRAD_ROWS / 16; u0 += 8) {
+        float t[8][4], sm[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int m = blockIdx.x * GRAD_ROWS + g + 16 * (u0 + u);
+            const typename E::mem *const at = dy + (size_t)m * (size_t)N + n;
+            sm[u] = big && m < M ? s[m] : 0.0f;
+            if (m < M && n + 4 <= N) {
+                load_piece<E, 4>(at, t[u]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[u][j] = m < M && n + j < N ? E::load(at[j]) : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                a[j] += t[u][j];
+                b[j] = fmaxf(b[j], fabsf(t[u][j] * sm[u]));
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        sums[g][c + j] = a[j];
+        bigs[g][c + j] = b[j];
+    }
+    __syncthreads();
+    const int col = threadIdx.x, at = blockIdx.y * 64 + col;
+    if (col < 64 && at < N) {
+        float x = sums[0][col], y = bigs[0][col];
+#pragma unroll
+        for (int w = 1; w < 16; ++w) {
+            x += sums[w][col];
+            y = fmaxf(y, bigs[w][col]);
+        }
+        if (sum) sum[(size_t)blockIdx.x * (size_t)N + at] = x;
+        if (big) big[(size_t)blockIdx.x * (size_t)N + at] = y;
+    }
+}
+
+// The blocks' results together: db[n] (sum != nullptr) and exps[n] (big != nullptr).  64 columns per workgroup, sixteen waves with every sixteenth
+// block each.
+template <typename E>
+__global__ __launch_bounds__(1024) void grad_columns_join_kernel(const float *__restrict__ sum, const float *__restrict__ big, typename E::mem *__restrict__ db,
+                                                                 int *__restrict__ exps, int blocks, int N) {
+    __shared__ float sums[16][64], bigs[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+    float x = 0.0f, y = 0.0f;
+    if (n < N) {
+#pragma unroll 4
+        for (int b = wave; b < blocks; b += 16) {
+            if (sum) x += sum[(size_t)b * (size_t)N + n];
+            if (big) y = fmaxf(y, big[(size_t)b * (size_t)N + n]);
+        }
+    }
+    sums[wave][lane] = x;
+    bigs[wave][lane] = y;
+    __syncthreads();
+    if (wave == 0 && n < N) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) {
+            x += sums[w][lane];
+            y = fmaxf(y, bigs[w][lane]);
+        }
+        if (sum) db[n] = E::store(x);
+        if (big) exps[n] = grad_exponent(y);
+    }
+}
+
+// 64 x 64 elements src[r][c] come out as out[c][..][r], padded with zeros to Rp rows: the transposed operands.  A workgroup holds the block in
 // LDS as floats; lanes read along c and write along r, 16 bytes a lane.
 constexpr int GRAD_LD = 65;
 template <typename Write>
@@ -81,15 +234,13 @@ __device__ __forceinline__ void grad_transposed(const float (&tile)[64][GRAD_LD]
     }
 }
 
-// out[n][z][m] = piece z of dy[m][n] * s[m] (PIECES), and on the way part[block][n] = sum of dy[m][n] over the block's 64 rows (part != nullptr).
-// Without PIECES the sums alone, the same ones.
-template <typename E, int P, bool PIECES>
-__global__ __launch_bounds__(256) void grad_split_columns_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, __bf16 *__restrict__ out,
-                                                                 float *__restrict__ part, int M, int N, int Mp) {
+// out[n][z][m] = piece z of dy[m][n] * s[m] 2^-exps[n]
+template <typename E, int P>
+__global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, const int *__restrict__ exps,
+                                                                        _Float16 *__restrict__ out, int M, int N, int Mp) {
     __shared__ float tile[64][GRAD_LD];
-    __shared__ float column[16][64];
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, c = (threadIdx.x & 15) * 4, n = c0 + c;
-    float t[4][4], sum[4] = {};
+    const int r0 = blockIdx.x * 64, c = (threadIdx.x & 15) * 4, n = blockIdx.y * 64 + c;
+    float t[4][4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int m = r0 + (threadIdx.x >> 4) + 16 * u;
@@ -104,61 +255,16 @@ __global__ __launch_bounds__(256) void grad_split_columns_kernel(const typename 
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int r = (threadIdx.x >> 4) + 16 * u, m = r0 + r;
-        const float sm = PIECES && m < M ? s[m] : 0.0f;
+        const float sm = m < M ? s[m] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            sum[j] += t[u][j];
-            if constexpr (PIECES) tile[r][c + j] = m < M && n + j < N ? t[u][j] * sm : 0.0f;
-        }
+        for (int j = 0; j < 4; ++j) tile[r][c + j] = m < M && n + j < N ? t[u][j] * sm : 0.0f;
     }
-    if (part)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) column[threadIdx.x >> 4][c + j] = sum[j];
     __syncthreads();
-    if constexpr (PIECES)
-        grad_transposed(tile, N, [&](int col, int row, const float(&e)[8]) {
-            bf16x8_t v[P];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                __bf16 q[P];
-                split_pieces<P>(e[j], q);
-#pragma unroll
-                for (int z = 0; z < P; ++z) v[z][j] = q[z];
-            }
-#pragma unroll
-            for (int z = 0; z < P; ++z) *reinterpret_cast<bf16x8_t *>(out + ((size_t)col * P + z) * (size_t)Mp + row) = v[z];
-        });
-    if (part && threadIdx.x < 64 && c0 + (int)threadIdx.x < N) {
-        float total = column[0][threadIdx.x];
-#pragma unroll
-        for (int g = 1; g < 16; ++g) total += column[g][threadIdx.x];
-        part[(size_t)blockIdx.x * (size_t)N + c0 + threadIdx.x] = total;
-    }
+    grad_transposed(tile, N, [&](int col, int row, const float(&e)[8]) { store_pieces<P>(e, exps[col], out + (size_t)col * P * (size_t)Mp + row, (size_t)Mp); });
 }
 
-// db[n] = the sum of the blocks' sums: 64 columns per workgroup, sixteen waves with every sixteenth block each
-template <typename E>
-__global__ __launch_bounds__(1024) void grad_bias_kernel(const float *__restrict__ part, typename E::mem *__restrict__ db, int blocks, int N) {
-    __shared__ float sum[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (n < N) {
-#pragma unroll 8
-        for (int b = wave; b < blocks; b += 16) s += part[(size_t)b * (size_t)N + n];
-    }
-    sum[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && n < N) {
-#pragma unroll
-        for (int w = 1; w < 16; ++w) s += sum[w][lane];
-        db[n] = E::store(s);
-    }
-}
-
-// out[c][z][r] = q[r][c] * 2^(-8 (copies - 1 - z))
-template <int P>
-__global__ __launch_bounds__(256) void grad_codes_kernel(const int8_t *__restrict__ q, __bf16 *__restrict__ out, int R, int C, int Rp) {
-    constexpr int Z = code_copies<P>;
+// out[c][r] = q[r][c]
+__global__ __launch_bounds__(GRAD_THREADS) void grad_codes_kernel(const int8_t *__restrict__ q, _Float16 *__restrict__ out, int R, int C, int Rp) {
     __shared__ float tile[64][GRAD_LD];
     const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
     const int rl = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16, r = r0 + rl;
@@ -177,14 +283,10 @@ __global__ __launch_bounds__(256) void grad_codes_kernel(const int8_t *__restric
     for (int j = 0; j < 16; ++j) tile[rl][c + j] = (float)(int8_t)(v[j / 4] >> (8 * (j % 4)));
     __syncthreads();
     grad_transposed(tile, C, [&](int col, int row, const float(&t)[8]) {
+        f16x8_t b;
 #pragma unroll
-        for (int z = 0; z < Z; ++z) {
-            const float f = z == Z - 1 ? 1.0f : (z == Z - 2 ? 0x1p-8f : 0x1p-16f);
-            bf16x8_t b;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) b[j] = (__bf16)(t[j] * f);
-            *reinterpret_cast<bf16x8_t *>(out + ((size_t)col * Z + z) * (size_t)Rp + row) = b;
-        }
+        for (int j = 0; j < 8; ++j) b[j] = (_Float16)t[j];
+        *reinterpret_cast<f16x8_t *>(out + (size_t)col * (size_t)Rp + row) = b;
     });
 }
 

@@ -1,4 +1,4 @@
-// The dense product of the token-wise operators, c[i][j] = sum over r of a[i][r] b[j][r], on rows of int8 codes or of bf16 numbers: both
+// The dense product of the token-wise operators, c[i][j] = sum over r of a[i][r] b[j][r], on rows of int8 codes or of fp16 numbers: both
 // matrix instructions take 16 bytes of a row per lane and 32 bytes per step, so one kernel in bytes serves both.
 #pragma once
 #include <type_traits>
@@ -12,14 +12,15 @@ typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x16_t __attribute__((ext_vector_type(16)));
 typedef float tile_f32x16_t __attribute__((ext_vector_type(16)));
 typedef float tile_f32x4_t __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int TILE_THREADS = 256;       // four waves, 2 x 2 over the tile
 
 struct TileParams {
     const char *a, *b;
     int I, J, Kb;               // Kb: bytes of a row that are summed over
-    int Kb_b;                   // bf16: bytes of a row of b (whole stages), which meets a's again and again
+    int Kb_b;                   // fp16: bytes of a row of b (whole stages), which meets a's again and again
+    const int *exp_i;           // fp16: a row of sums is worth times 2^exp_i
     uint32_t lda, ldb;          // bytes from row to row
     int tiles_i, tiles_j;
     // int8: rescaling by row and column, bias, activation
@@ -35,11 +36,11 @@ struct TileI8 {
     static constexpr bool INT = true;
     static __device__ __forceinline__ acc_t mfma(i32x4_t a, i32x4_t b, acc_t c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
-struct TileBF16 {
+struct TileF16 {
     typedef tile_f32x16_t acc_t;
     static constexpr bool INT = false;
     static __device__ __forceinline__ acc_t mfma(i32x4_t a, i32x4_t b, acc_t c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
     }
 };
 
@@ -105,7 +106,8 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
     constexpr int TURN = 2 * TM * ((TN / 2 * (int)sizeof(typename E::mem) < 256 ? TN / 2 * (int)sizeof(typename E::mem) : 256) + 16);
     constexpr int LDS_BYTES = NB * STAGE > TURN ? NB * STAGE : TURN;
     __shared__ __align__(1024) char lds[LDS_BYTES];
-    __shared__ __align__(16) float side[Op::INT ? TM + 2 * TN : 4];     // s_i, s_j, bias of the tile
+    constexpr int SIDE_N = Op::INT ? TM + 2 * TN : TM;
+    __shared__ __align__(16) float side[SIDE_N];            // s_i, s_j, bias of the tile, or the bits of exp_i
     typedef __attribute__((address_space(3))) void *lds_ptr_t;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj;
@@ -113,16 +115,18 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
     const int i0 = (int)ti * TM, j0 = (int)tj * TN;
     const int wi = (wave & 1) * (TM / 2), wj = (wave >> 1) * (TN / 2);
 
-    constexpr int SIDE = (TM + 2 * TN + TILE_THREADS - 1) / TILE_THREADS;
+    constexpr int SIDE = (SIDE_N + TILE_THREADS - 1) / TILE_THREADS;
     float side_v[SIDE];                     // (requested now, put into LDS when the sums are done)
-    if constexpr (Op::INT) {
 #pragma unroll
-        for (int u = 0; u < SIDE; ++u) {
-            const int x = u * TILE_THREADS + (int)threadIdx.x;
-            side_v[u] = 0.0f;
+    for (int u = 0; u < SIDE; ++u) {
+        const int x = u * TILE_THREADS + (int)threadIdx.x;
+        side_v[u] = 0.0f;
+        if constexpr (Op::INT) {
             if (x < TM) side_v[u] = p.s_i[min(i0 + x, p.I - 1)];
             else if (x < TM + TN) side_v[u] = p.s_j[min(j0 + x - TM, p.J - 1)];
             else if (x < TM + 2 * TN && p.bias) side_v[u] = p.bias[min(j0 + x - TM - TN, p.J - 1)];
+        } else {
+            if (x < TM) side_v[u] = __int_as_float(p.exp_i[min(i0 + x, p.I - 1)]);
         }
     }
 
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
     typename Op::acc_t acc[BI][BJ] = {};
 
     const int full = Kb / SB, rest = Kb - full * SB;
-    const int total = full + (rest ? 1 : 0);        // (rows of bf16 are made in whole stages)
+    const int total = full + (rest ? 1 : 0);        // (rows of fp16 are made in whole stages)
 
     if constexpr (DMA) {
         int dma_s = 0;          // stage that is requested next
@@ -313,11 +317,9 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
     constexpr int ROW = CB * SIZE + 16;                            // (rows start in different banks)
     constexpr int PL = piece_len<E>, LANES = CB / PL;              // lanes that store a row
     static_assert(4 * WI * ROW <= LDS_BYTES, "the turned outputs of four waves");
-    if constexpr (Op::INT) {
 #pragma unroll
-        for (int u = 0; u < SIDE; ++u)
-            if (u * TILE_THREADS + (int)threadIdx.x < TM + 2 * TN) side[u * TILE_THREADS + threadIdx.x] = side_v[u];
-    }
+    for (int u = 0; u < SIDE; ++u)
+        if (u * TILE_THREADS + (int)threadIdx.x < SIDE_N) side[u * TILE_THREADS + threadIdx.x] = side_v[u];
     __syncthreads();                        // (and every wave has read its last fragments)
     char *const turn = lds + wave * (WI * ROW);
     typename E::mem *const c = static_cast<typename E::mem *>(p.c) + (size_t)blockIdx.y * (size_t)p.I * (size_t)p.J;
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
     for (int cb = 0; cb < WJ / CB; ++cb) {
 #pragma unroll
         for (int bi = 0; bi < BI; ++bi) {
-            const float s_i = Op::INT ? side[wi + 32 * bi + (lane & 31)] : 0.0f;
+            const float s_i = side[wi + 32 * bi + (lane & 31)];
 #pragma unroll
             for (int bj = cb * (CB / 32); bj < (cb + 1) * (CB / 32); ++bj) {
 #pragma unroll
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
                         for (int v = 0; v < 4; ++v) y[v] = int8_finish<TANH>(acc[bi][bj][4 * g + v], s_i, sv[v], bv[v], floor, p.act);
                     } else {
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) y[v] = acc[bi][bj][4 * g + v];
+                        for (int v = 0; v < 4; ++v) y[v] = __builtin_amdgcn_ldexpf(acc[bi][bj][4 * g + v], __float_as_int(s_i));
                     }
                     typedef typename E::mem quad_t __attribute__((ext_vector_type(4)));
                     *reinterpret_cast<quad_t *>(turn + (32 * bi + (lane & 31)) * ROW + (col - cb * CB) * SIZE) =

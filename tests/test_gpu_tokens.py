@@ -4,8 +4,9 @@ embedding and its gradient, dropout.
 Tolerances.  Steps that the header orders one by one (quantiser, product with its finish, lookup, dropout) are compared bit for bit:
 the oracle takes the same fp32 steps, and the last rounding to fp16 / bf16 is the nearest one.  Sums of floats are compared with sums in
 64 bits: with u = 2^-24, fp32 sums of R terms in any order are within (R + 2) u * sum |term| (a rounding per addition, two to form
-a term), a 16-bit result adds half a step of its type (eps / 2 of the value, or half of its smallest subnormal), and a gradient
-of the product on a 16-bit type keeps 16 bits of dy * s: 2^-17 * sum |term| more."""
+a term), and a 16-bit result adds half a step of its type (eps / 2 of the value, or half of its smallest subnormal).  Gradients of the
+product keep dy * s to 22 bits (two fp16 numbers, each within 2^-11 of what it stands for: 2^-22 of a term) or, for bf16, to 11 (one:
+2^-11), and never worse than 2^-40 of the largest dy * s of the sum, which counts once for every code it meets."""
 import numpy as np
 import pytest
 
@@ -16,6 +17,7 @@ pytestmark = pytest.mark.gpu
 
 TYPES = ("f32", "f16", "bf16")
 U = 2.0 ** -24
+KEPT = {"f32": 2.0 ** -22, "f16": 2.0 ** -22, "bf16": 2.0 ** -11}
 
 
 def _t(name):
@@ -54,12 +56,17 @@ def same_bits(got, want):
     assert ok.all(), (int((~ok).sum()), got.shape, np.argwhere(~ok)[:4].tolist(), g[~ok][:4], w[~ok][:4])
 
 
-def within(got, want, mass, terms, name, kept=0.0):
-    """|got - want| <= bound of the module text; mass: sum of |terms|"""
+def far_below(t, q):
+    """What elements far below the largest of their row t[i] may lose in all: 2^-40 of it for every unit of the codes q [r][j]"""
+    return 2.0 ** -40 * np.abs(t.astype(np.float64)).max(axis=1, initial=0.0)[:, None] * np.abs(q.astype(np.float64)).sum(axis=0)[None, :]
+
+
+def within(got, want, mass, terms, name, kept=0.0, lost=0.0):
+    """|got - want| <= bound of the module text; mass: sum of |terms|; lost: far_below"""
     import torch
     fi = torch.finfo(_t(name))
     got = f64(got)
-    bound = ((terms + 2) * U + kept) * mass + 2.0 ** -149 * (terms + 2)
+    bound = ((terms + 2) * U + kept) * mass + lost + 2.0 ** -149 * (terms + 2)
     if name != "f32":
         bound = bound * (1 + fi.eps) + fi.eps / 2 * np.abs(want) + fi.smallest_normal * fi.eps / 2
     bad = ~(np.abs(got - want) <= bound)
@@ -247,9 +254,8 @@ def test_int8_linear_backward(B, name, M, K, N):
     dy, dyd = randn(rng, (M, N), name)
     dx, dw, db = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w))
     (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(dy, a, s_a, w, s_w)
-    kept = 0.0 if name == "f32" else 2.0 ** -17
-    within(dx, wx, mx, N, name, kept)
-    within(dw, ww, mw, M, name, kept)
+    within(dx, wx, mx, N, name, KEPT[name], far_below(dy * s_w, w))
+    within(dw, ww, mw, M, name, KEPT[name], far_below((dy * s_a[:, None]).T, a))
     within(db, wb, mb, M, name)
     # the same call again: the same bits; each gradient alone: the same bits
     dx2, dw2, db2 = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w), want=("dx",)) [0], \
@@ -271,9 +277,39 @@ def test_int8_linear_backward_over_the_range_of_fp32(B, exponent):
     dx, dw, db = B.adapt_int8_linear_backward(dev(dy), dev(a), dev(s_a), dev(w), dev(s_w))
     # forming dy * s may round a subnormal: half of 2^-149 for each term, times a code of up to 128
     (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(dy, a, s_a, w, s_w)
-    within(dx, wx, mx + N * 128 * 2.0 ** -125, N, "f32")
-    within(dw, ww, mw + M * 128 * 2.0 ** -125, M, "f32")
+    within(dx, wx, mx + N * 128 * 2.0 ** -125, N, "f32", KEPT["f32"], far_below(dy * s_w, w))
+    within(dw, ww, mw + M * 128 * 2.0 ** -125, M, "f32", KEPT["f32"], far_below((dy * s_a[:, None]).T, a))
     within(db, wb, mb, M, "f32")
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_int8_linear_backward_rows_of_very_different_elements(B, name):
+    """One element of a row (column) dwarfs the others and meets a code of 0: what is left of the sum still keeps its bits."""
+    rng = np.random.default_rng(31)
+    M, K, N = 130, 70, 200
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    dy = rng.standard_normal((M, N)) * 1e-4
+    loud = rng.integers(0, N, M)
+    dy[np.arange(M), loud] = 1.0
+    w[:, :20] = np.where(rng.random((N, 20)) < 0.5, 0, w[:, :20])
+    dy, dyd = (lambda t: (t.float().numpy(), t.cuda()))(rounded(dy.astype(np.float32), name))
+    dx, dw, _ = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w))
+    (wx, mx), (ww, mw), _ = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+    within(dx, wx, mx, N, name, KEPT[name], far_below(dy * s_w, w))
+    within(dw, ww, mw, M, name, KEPT[name], far_below((dy * s_a[:, None]).T, a))
+
+
+@pytest.mark.parametrize("M,K,N", [(5, 40, 9000), (9000, 40, 5), (70, 33, 2100), (2100, 33, 70), (66, 20, 1100), (300, 16, 4500), (3, 5, 600)])
+def test_int8_linear_backward_long_sums(B, M, K, N):
+    rng = np.random.default_rng(M)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    for name in ("f32", "bf16"):
+        dy, dyd = randn(rng, (M, N), name)
+        dx, dw, db = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w))
+        (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+        within(dx, wx, mx, N, name, KEPT[name], far_below(dy * s_w, w))
+        within(dw, ww, mw, M, name, KEPT[name], far_below((dy * s_a[:, None]).T, a))
+        within(db, wb, mb, M, name)
 
 
 def test_int8_linear_backward_infinities_and_nan_stay_in_their_rows(B):
@@ -480,8 +516,7 @@ def test_a_training_step_of_the_text_path(B, name, T, V, D, N):
     assert (got["a"].cpu().numpy() == a).all() and (got["s_a"].cpu().numpy() == s_a).all()
     same_bits(got["y"], rounded(ot.int8_linear(a, s_a, h["w"], h["s_w"], h["bias"]), name))
     (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(h["dy"], a, s_a, h["w"], h["s_w"])
-    kept = 0.0 if name == "f32" else 2.0 ** -17
-    within(got["dw"], ww, mw, T, name, kept)
+    within(got["dw"], ww, mw, T, name, KEPT[name], far_below((h["dy"] * s_a[:, None]).T, a))
     within(got["db"], wb, mb, T, name)
     want, mass, n = ot.embedding_backward(got["de"].float().cpu().numpy(), h["tok"], V, 2.0, 0)
     within(got["dt"], want, mass, n[:, None], name)
@@ -588,7 +623,7 @@ def test_int8_linear_backward_beyond_32_bits(B, big):
     dx, _, _ = B.adapt_int8_linear_backward(dyd, a, torch.ones(M, device="cuda"), dev(w), dev(s_w), want=("dx",))
     for rows in (slice(0, 3), slice(1022600, 1022610), slice(M - 3, M)):
         (want, mass), _, _ = ot.int8_linear_backward(dy[rows], np.zeros((dy[rows].shape[0], K), np.int8), np.ones(dy[rows].shape[0], np.float32), w, s_w)
-        within(dx[rows], want, mass, N, "bf16", 2.0 ** -17)
+        within(dx[rows], want, mass, N, "bf16", KEPT["bf16"], far_below(dy[rows] * s_w, w))
 
 
 def test_embedding_beyond_32_bits(B, big):
