@@ -890,6 +890,14 @@ def _new(stream, like, shape, dtype):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _result(what, t, stream, like, shape, dtype, here):
+    """The caller's tensor or a new one, and its address."""
+    if t is None:
+        t = _new(stream, like, shape, dtype)
+        return t, t.data_ptr()
+    return t, _arg(what, t, dtype, shape, here)
+
+
 def _workspace(workspace, need, stream, like, here):
     """The caller's uint8 tensor if it is large enough, else a new one, which the calling function holds until its kernels are enqueued."""
     if workspace is not None:
@@ -904,12 +912,9 @@ def adapt_quantize_tokens(x, bits: int = 8, out=None, scales=None, stream=None):
     tokens, cols = x.shape
     here = _here()
     px = _arg("x", x, x.dtype, (tokens, cols), here)
-    if out is None:
-        out = _new(stream, x, (tokens, cols), torch.int8)
-    if scales is None:
-        scales = _new(stream, x, (tokens,), torch.float32)
-    _chk(load().adapt_quantize_tokens(px, _element(x.dtype), _arg("out", out, torch.int8, (tokens, cols), here),
-                                      _arg("scales", scales, torch.float32, (tokens,), here), tokens, cols, bits, _raw_stream(stream, here)))
+    out, pout = _result("out", out, stream, x, (tokens, cols), torch.int8, here)
+    scales, pscales = _result("scales", scales, stream, x, (tokens,), torch.float32, here)
+    _chk(load().adapt_quantize_tokens(px, _element(x.dtype), pout, pscales, tokens, cols, bits, _raw_stream(stream, here)))
     return out, scales
 
 
@@ -919,14 +924,13 @@ def adapt_int8_linear(a, s_a, w, s_w, bias=None, act: int = 0, dtype=torch.float
     N = w.shape[0]
     here = _here()
     pa = _arg("a", a, torch.int8, (M, K), here)
-    if out is None:
-        out = _new(stream, a, (M, N), dtype)
-    else:
+    if out is not None:
         dtype = out.dtype
+    out, pout = _result("out", out, stream, a, (M, N), dtype, here)
     _chk(load().adapt_int8_linear(pa, _arg("s_a", s_a, torch.float32, (M,), here), _arg("w", w, torch.int8, (N, K), here),
                                   _arg("s_w", s_w, torch.float32, (N,), here),
                                   None if bias is None else _arg("bias", bias, torch.float32, (N,), here), act,
-                                  _arg("out", out, dtype, (M, N), here), _element(dtype), M, K, N, _raw_stream(stream, here)))
+                                  pout, _element(dtype), M, K, N, _raw_stream(stream, here)))
     return out
 
 
@@ -965,10 +969,9 @@ def adapt_embedding(table, tokens, scale: float = 1.0, out=None, stream=None):
     tok, tok_bits = _tokens(tokens, here)
     pt = _arg("table", table, table.dtype, (V, D), here)
     shape = (*tokens.shape, D)
-    if out is None:
-        out = _new(stream, table, shape, table.dtype)
-    _chk(load().adapt_embedding(pt, _element(table.dtype), tok, tok_bits, _arg("out", out, table.dtype, shape, here), tokens.numel(), V, D,
-                                scale, _raw_stream(stream, here)))
+    out, pout = _result("out", out, stream, table, shape, table.dtype, here)
+    _chk(load().adapt_embedding(pt, _element(table.dtype), tok, tok_bits, pout, tokens.numel(), V, D, scale,
+                                _raw_stream(stream, here)))
     return out
 
 
@@ -980,9 +983,7 @@ def adapt_embedding_backward(dy, tokens, V: int, scale: float = 1.0, padding_idx
     tok, tok_bits = _tokens(tokens, here)
     pdy = _arg("dy", dy, dy.dtype, (*tokens.shape, D), here)
     e = _element(dy.dtype)
-    if out is None:
-        out = _new(stream, dy, (V, D), dy.dtype)
-    pout = _arg("out", out, dy.dtype, (V, D), here)
+    out, pout = _result("out", out, stream, dy, (V, D), dy.dtype, here)
     need = ctypes.c_size_t(0)
     _chk(load().adapt_embedding_backward_workspace(tokens.numel(), V, D, ctypes.byref(need)))
     ws = _workspace(workspace, need.value, stream, dy, here)
@@ -995,9 +996,8 @@ def _dropout(call, x, p, seed, offset, step, out, stream):
     here = _here()
     px = _arg("x", x, x.dtype, x.shape, here)
     e = _element(x.dtype)
-    if out is None:
-        out = _new(stream, x, x.shape, x.dtype)
-    _chk(call(px, _arg("out", out, x.dtype, x.shape, here), e, x.numel(), p, seed, offset,
+    out, pout = _result("out", out, stream, x, x.shape, x.dtype, here)
+    _chk(call(px, pout, e, x.numel(), p, seed, offset,
               None if step is None else _arg("step", step, torch.int64, (1,), here), _raw_stream(stream, here)))
     return out
 

@@ -8,8 +8,8 @@
 // two, t = t0 + t1, t1 the rest that t0 leaves (22 bits: fp16 and fp32 gradients; 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at
 // every addition).  Elements below 2^-18 (22 bits) or 2^-29 (11 bits) of their row's largest keep fewer bits; what they lose is below 2^-40 of that largest.  So a
 // gradient is an fp16 product with exact partial products and fp32 sums over rows [t1 | t0] that meet the same codes twice, the small pieces first.
-// (Three bf16 pieces of 24 bits, without the rows' powers of two, took 148 us where this takes SEQ for 6400 x 512 -> 2048 fp32; two of them 470 us
-// against BIG for 4096^3 bf16.)
+// (Three bf16 pieces of 24 bits, without the rows' powers of two, took 148 us where this takes 124 for 6400 x 512 -> 2048 fp32; two of them 470 us
+// against 287 for 4096^3 bf16.)
 //
 // Both matrices are written to the workspace with the summed index last, rows in whole stages of 128 bytes.
 #pragma once
@@ -137,40 +137,41 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_long_rows_kernel(const type
     }
 }
 
-// Of every column n over GRAD_ROWS rows: sum[block][n] of dy (sum != nullptr), big[block][n] = max |dy s| (big != nullptr).  Sixteen threads per
-// four columns, every sixteenth row each.
+// Of every column n over GRAD_ROWS rows: sum[block][n] of dy (sum != nullptr), big[block][n] = max |dy s| (big != nullptr).  A thread takes 16
+// bytes of every 16th (32nd) row.
 constexpr int GRAD_ROWS = 256;
 template <typename E>
 __global__ __launch_bounds__(GRAD_THREADS) void grad_columns_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, float *__restrict__ sum,
                                                                     float *__restrict__ big, int M, int N) {
-    __shared__ float sums[16][64], bigs[16][64];
-    const int c = (threadIdx.x & 15) * 4, n = blockIdx.y * 64 + c, g = threadIdx.x >> 4;
-    float a[4] = {}, b[4] = {};
+    constexpr int P = piece_len<E>, LANES = 64 / P, G = GRAD_THREADS / LANES;
+    __shared__ float sums[G][64], bigs[G][64];
+    const int c = (threadIdx.x % LANES) * P, n = blockIdx.y * 64 + c, g = threadIdx.x / LANES;
+    float a[P] = {}, b[P] = {};
 #pragma unroll
-    for (int u0 = 0; u0 < GRAD_ROWS / 16; u0 += 8) {
-        float t[8][4], sm[8];
+    for (int u0 = 0; u0 < GRAD_ROWS / G; u0 += 8) {
+        float t[8][P], sm[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int m = blockIdx.x * GRAD_ROWS + g + 16 * (u0 + u);
+            const int m = blockIdx.x * GRAD_ROWS + g + G * (u0 + u);
             const typename E::mem *const at = dy + (size_t)m * (size_t)N + n;
             sm[u] = big && m < M ? s[m] : 0.0f;
-            if (m < M && n + 4 <= N) {
-                load_piece<E, 4>(at, t[u]);
+            if (m < M && n + P <= N) {
+                load_piece<E, P>(at, t[u]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t[u][j] = m < M && n + j < N ? E::load(at[j]) : 0.0f;
+                for (int j = 0; j < P; ++j) t[u][j] = m < M && n + j < N ? E::load(at[j]) : 0.0f;
             }
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < P; ++j) {
                 a[j] += t[u][j];
                 b[j] = fmaxf(b[j], fabsf(t[u][j] * sm[u]));
             }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < P; ++j) {
         sums[g][c + j] = a[j];
         bigs[g][c + j] = b[j];
     }
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_columns_kernel(const typena
     if (col < 64 && at < N) {
         float x = sums[0][col], y = bigs[0][col];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) {
+        for (int w = 1; w < G; ++w) {
             x += sums[w][col];
             y = fmaxf(y, bigs[w][col]);
         }
