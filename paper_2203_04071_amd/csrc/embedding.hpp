@@ -13,6 +13,11 @@ __device__ __forceinline__ uint32_t embed_row(Tok t, uint32_t V) {
     return t >= 0 && (uint64_t)t < (uint64_t)V ? (uint32_t)t : V;
 }
 
+// Where the piece of P elements at c of a row of D is taken: the last one ends with the row, and does again what the one before it does in part
+// (the same numbers, written twice).  Rows shorter than a piece: element by element.
+template <int P>
+__device__ __forceinline__ uint32_t embed_piece(uint32_t c, uint32_t D) { return c + P <= D || D < P ? c : D - P; }
+
 // 2^lg lanes share a row, in pieces of 16 bytes
 template <typename E, typename Tok>
 __global__ __launch_bounds__(EMB_THREADS) void embedding_kernel(const typename E::mem *__restrict__ table, const Tok *__restrict__ tokens,
@@ -25,14 +30,15 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_kernel(const typename E
         const typename E::mem *const from = table + (size_t)(v < V ? v : 0) * D;
         typename E::mem *const to = y + t * D;
         for (uint32_t c = lane * P; c < D; c += P << lg) {
-            if (c + P <= D) {
+            const uint32_t at = embed_piece<P>(c, D);
+            if (at + P <= D) {
                 float f[P];
-                if (v < V) load_piece<E, P>(from + c, f);
+                if (v < V) load_piece<E, P>(from + at, f);
 #pragma unroll
                 for (int i = 0; i < P; ++i) f[i] = v < V ? f[i] * scale : 0.0f;
-                store_piece<E, P>(to + c, f);
+                store_piece<E, P>(to + at, f);
             } else {
-                for (uint32_t i = c; i < D; ++i) to[i] = E::store(v < V ? E::load(from[i]) * scale : 0.0f);
+                for (uint32_t i = at; i < D; ++i) to[i] = E::store(v < V ? E::load(from[i]) * scale : 0.0f);
             }
         }
     }
@@ -274,10 +280,11 @@ __device__ __forceinline__ void embed_empty_rows(const EmbedSum &p, typename E::
         const uint32_t rows_on = 64 / pieces, pieces_on = 64 % pieces;
         while (row < EMB_ZERO_ROWS) {
             if ((absent >> row) & 1) {
-                typename E::mem *const to = rows + (size_t)row * p.D + piece * P;
-                if (piece * P + P <= p.D) store_piece<E, P>(to, zero);
+                const uint32_t at = embed_piece<P>(piece * P, p.D);
+                typename E::mem *const to = rows + (size_t)row * p.D;
+                if (at + P <= p.D) store_piece<E, P>(to + at, zero);
                 else
-                    for (uint32_t i = piece * P; i < p.D; ++i) to[i - piece * P] = E::store(0.0f);
+                    for (uint32_t i = at; i < p.D; ++i) to[i] = E::store(0.0f);
             }
             row += rows_on;
             piece += pieces_on;
@@ -300,7 +307,8 @@ __global__ __launch_bounds__(EMB_THREADS) void embed_sum_kernel(const EmbedSum p
     const uint32_t piece = blockIdx.x * per + (threadIdx.x >> p.lg);
     if (piece >= p.pieces) return;
     const uint32_t first = piece * p.C, last = min(first + p.C, p.T);       // (pieces cover T: first < T)
-    for (uint32_t c = lane * P; c < p.D; c += (uint32_t)P << p.lg) {
+    for (uint32_t c0 = lane * P; c0 < p.D; c0 += (uint32_t)P << p.lg) {
+        const uint32_t c = embed_piece<P>(c0, p.D);
         const int len = (int)min((uint32_t)P, p.D - c);
         float acc[P] = {};
         uint32_t key = p.key[first];
@@ -312,7 +320,7 @@ __global__ __launch_bounds__(EMB_THREADS) void embed_sum_kernel(const EmbedSum p
                 if (len == P) store_piece<F32, P>(part, acc);
                 else
                     for (int j = 0; j < len; ++j) part[j] = acc[j];
-                if (!open && c == 0) {
+                if (!open && c0 == 0) {
                     const bool many = piece + EMB_LONG < p.pieces && p.key[(piece + EMB_LONG) * p.C] == key;
                     const uint32_t at = atomicAdd(&p.runs[many], 1u);
                     p.run[many ? p.pieces - 1 - at : at] = piece;
