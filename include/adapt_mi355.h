@@ -554,7 +554,7 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
  * dw_dev, db_dev may be NULL (not computed; a_dev and s_a_dev are read for dw alone, w_dev and s_w_dev for dx alone).  They are
  * fully overwritten.  dy * s is formed in fp32 and kept to 22 bits (ADAPT_F32, ADAPT_F16) or 11 bits (ADAPT_BF16, whose results keep 8), elements
  * far below the largest of their sum's to 2^-40 of that largest; sums are fp32.
- * M, K and N are at most 2^21 and no matrix has 2^36 elements, else ADAPT_ERR_UNSUPPORTED.
+ * M, K and N are at most 2^21 and no matrix has 2^34 elements, else ADAPT_ERR_UNSUPPORTED.
  * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
  * dx_dev / dw_dev are given). */
 int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes);

@@ -144,9 +144,13 @@ GradPlan grad_plan(long long I, long long J, long long R, int P) {
 }
 int grad_pieces(int type) { return type == ADAPT_BF16 ? 1 : 2; }
 
-// rows of partial results of the columns: sums, largest elements
-size_t column_blocks(int M) { return ((size_t)M + adapt::GRAD_ROWS - 1) / adapt::GRAD_ROWS; }
-size_t column_bytes(int M, int N) { return 2 * round256((M ? column_blocks(M) : 1) * (size_t)N * 4); }
+// partial results of the columns, sums and largest elements: rows that a block takes, blocks, bytes
+int column_rows(int M) {
+    const int share = (M + adapt::GRAD_BLOCKS - 1) / adapt::GRAD_BLOCKS;
+    return share <= adapt::GRAD_ROWS ? adapt::GRAD_ROWS : (share + adapt::GRAD_ROWS - 1) / adapt::GRAD_ROWS * adapt::GRAD_ROWS;
+}
+int column_blocks(int M) { return (int)((M + (long long)column_rows(M) - 1) / column_rows(M)); }
+size_t column_bytes(int M, int N) { return 2 * round256((size_t)(M ? column_blocks(M) : 1) * (size_t)N * 4); }
 
 template <class E>
 void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_t s) {
@@ -172,49 +176,72 @@ void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_
     }
 }
 
-dim3 blocks64(int R, int C) { return dim3((unsigned)((R + 63) / 64), (unsigned)((C + 63) / 64)); }
-
-// a wave per row up to 2048 elements, a workgroup up to 8192 (quantize_tokens has the same rule); a workgroup takes several rows, whose scales
-// of the columns it reads once
+// a wave per row up to 1024 elements, a workgroup up to 8192 (quantize_tokens has the like); a workgroup takes several rows, whose scales of the
+// columns it reads once
 template <class E, int P>
-void grad_rows(const typename E::mem *dy, const float *s_w, _Float16 *a, int *exps, int M, int N, int Np, hipStream_t s) {
+void prepare(const adapt::GradPrep &p, unsigned groups, hipStream_t s) {
     constexpr int T = adapt::GRAD_THREADS;
-    const unsigned by_wave = (unsigned)((M + 3) / 4 < 2048 ? (M + 3) / 4 : 2048), by_group = (unsigned)(M < 2048 ? M : 2048);
-    if (Np <= 512) adapt::grad_rows_kernel<E, P, 64, 1><<<by_wave, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
-    else if (Np <= 1024) adapt::grad_rows_kernel<E, P, 64, 2><<<by_wave, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
-    else if (Np <= 2048) adapt::grad_rows_kernel<E, P, T, 1><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
-    else if (Np <= 4096) adapt::grad_rows_kernel<E, P, T, 2><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
-    else if (Np <= 8192) adapt::grad_rows_kernel<E, P, T, 4><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
-    else adapt::grad_long_rows_kernel<E, P><<<by_group, T, 0, s>>>(dy, s_w, a, exps, M, N, Np);
+    if (p.Np <= 512) adapt::grad_prepare_kernel<E, P, 64, 1><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 1024) adapt::grad_prepare_kernel<E, P, 64, 2><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 2048) adapt::grad_prepare_kernel<E, P, T, 1><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 4096) adapt::grad_prepare_kernel<E, P, T, 2><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 8192) adapt::grad_prepare_kernel<E, P, T, 4><<<groups, T, 0, s>>>(p);
+    else adapt::grad_prepare_kernel<E, P, 0, 0><<<groups, T, 0, s>>>(p);
 }
 
+// Workspace: what dx needs, what dw needs, the columns' partial results.
 template <class E, int P>
-void gradients(const adapt::Int8Params &q, const void *dy_dev, void *dx, void *dw, void *db, char *ws, hipStream_t s) {
+void gradients(const adapt::Int8Params &q, const void *dy, void *dx, void *dw, void *db_dev, char *ws, hipStream_t s) {
     typedef typename E::mem mem;
-    const mem *const dy = static_cast<const mem *>(dy_dev);
-    _Float16 *const a = reinterpret_cast<_Float16 *>(ws);
+    mem *const db = static_cast<mem *>(db_dev);
+    const GradPlan gx = dx ? grad_plan(q.M, q.K, q.N, P) : GradPlan{}, gw = dw ? grad_plan(q.N, q.K, q.M, P) : GradPlan{};
+    char *const wx = ws, *const ww = ws + gx.bytes, *const wc = ww + gw.bytes;
+    auto blocks = [](int n) { return (uint32_t)((n + 63) / 64); };
+    adapt::GradPrep p{};
+    p.dy = dy;
+    p.s_a = q.s_a;
+    p.s_w = q.s_w;
+    p.a = q.a;
+    p.w = q.w;
+    p.M = q.M;
+    p.K = q.K;
+    p.N = q.N;
+    p.Np = gx.Rp;
+    p.Mp = gw.Rp;
+    p.rows = column_rows(q.M);
+    p.dy_rows = reinterpret_cast<_Float16 *>(wx);
+    p.w_codes = reinterpret_cast<_Float16 *>(wx + gx.b);
+    p.row_exps = reinterpret_cast<int *>(wx + gx.exps);
+    p.a_codes = reinterpret_cast<_Float16 *>(ww + gw.b);
+    p.sum = db ? reinterpret_cast<float *>(wc) : nullptr;
+    p.big = dw ? reinterpret_cast<float *>(wc + column_bytes(q.M, q.N) / 2) : nullptr;
     if (dx) {
-        const GradPlan g = grad_plan(q.M, q.K, q.N, P);
-        grad_rows<E, P>(dy, q.s_w, a, reinterpret_cast<int *>(ws + g.exps), q.M, q.N, g.Rp, s);
-        if (g.Rp) adapt::grad_codes_kernel<<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.w, reinterpret_cast<_Float16 *>(ws + g.b), q.N, q.K, g.Rp);
-        grad_product<E>(g, ws, q.M, q.K, dx, s);
+        const uint32_t rows = p.Np <= 1024 ? ((uint32_t)q.M + 3) / 4 : (uint32_t)q.M;
+        p.row_groups = rows < 2048 ? rows : 2048;
+        p.w_blocks = (uint32_t)gx.Rp / 64;
+        p.w_groups = p.w_blocks * blocks(q.K);
     }
     if (dw || db) {
-        const GradPlan g = dw ? grad_plan(q.N, q.K, q.M, P) : GradPlan{};
-        const int blocks = (int)column_blocks(q.M);
-        float *const sum = db ? reinterpret_cast<float *>(ws + g.bytes) : nullptr;
-        float *const big = dw ? reinterpret_cast<float *>(ws + g.bytes + column_bytes(q.M, q.N) / 2) : nullptr;
-        int *const exps = reinterpret_cast<int *>(ws + g.exps);
-        if (blocks) adapt::grad_columns_kernel<E><<<dim3((unsigned)blocks, (unsigned)((q.N + 63) / 64)), 256, 0, s>>>(dy, q.s_a, sum, big, q.M, q.N);
-        adapt::grad_columns_join_kernel<E><<<(unsigned)((q.N + 63) / 64), 1024, 0, s>>>(sum, big, static_cast<mem *>(db), exps, blocks, q.N);
-        if (dw) {
-            if (g.Rp) {
-                adapt::grad_turned_rows_kernel<E, P><<<blocks64(g.Rp, q.N), 256, 0, s>>>(dy, q.s_a, exps, a, q.M, q.N, g.Rp);
-                adapt::grad_codes_kernel<<<blocks64(g.Rp, q.K), 256, 0, s>>>(q.a, reinterpret_cast<_Float16 *>(ws + g.b), q.M, q.K, g.Rp);
-            }
-            grad_product<E>(g, ws, q.N, q.K, dw, s);
-        }
+        p.column_blocks = (uint32_t)column_blocks(q.M);
+        p.column_groups = p.column_blocks * blocks(q.N);
     }
+    uint32_t a_groups = 0;
+    if (dw) {
+        p.a_blocks = (uint32_t)gw.Rp / 64;
+        a_groups = p.a_blocks * blocks(q.K);
+    }
+    const uint32_t groups = p.row_groups + p.w_groups + p.column_groups + a_groups;
+    if (groups) prepare<E, P>(p, groups, s);
+    if (dx) grad_product<E>(gx, wx, q.M, q.K, dx, s);
+    if (dw && gw.Rp) {
+        adapt::grad_turned_rows_kernel<E, P><<<dim3((unsigned)gw.Rp / 64, blocks(q.N)), 256, 0, s>>>(
+            static_cast<const mem *>(dy), q.s_a, p.sum, p.big, db, reinterpret_cast<int *>(ww + gw.exps), reinterpret_cast<_Float16 *>(ww), q.M, q.N, gw.Rp,
+            column_blocks(q.M));
+    } else {
+        if (dw) adapt::fill_u32_kernel<<<ew_grid((size_t)q.N), 256, 0, s>>>(reinterpret_cast<uint32_t *>(ww + gw.exps), 0u, (size_t)q.N);
+        if (db) adapt::grad_bias_kernel<E><<<blocks(q.N), adapt::GRAD_THREADS, 0, s>>>(p.sum, db, column_blocks(q.M), q.N);
+    }
+    if (dw) grad_product<E>(gw, ww, q.N, q.K, dw, s);
 }
 
 }  // namespace
@@ -247,13 +274,11 @@ int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want
     if (int rc = int8_args(who, M, K, N, type)) return rc;
     const int P = grad_pieces(type);
     if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
-    if ((long long)M * K >> 36 || (long long)N * K >> 36 || (long long)M * N >> 36) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a matrix of 2^36 elements or more", who);
-    size_t need = column_bytes(M, N);       // partial results of the columns: behind what dw needs
+    // (three matrices in blocks of 64 x 64, a workgroup of 256 each, in one launch of less than 2^32 threads)
+    if ((long long)M * K >> 34 || (long long)N * K >> 34 || (long long)M * N >> 34) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a matrix of 2^34 elements or more", who);
+    size_t need = column_bytes(M, N);
     if (want_dw && N && K) need += grad_plan(N, K, M, P).bytes;
-    if (want_dx && M && K) {
-        const size_t b = grad_plan(M, K, N, P).bytes;
-        need = b > need ? b : need;
-    }
+    if (want_dx && M && K) need += grad_plan(M, K, N, P).bytes;
     *bytes = need;
     return ADAPT_OK;
 }

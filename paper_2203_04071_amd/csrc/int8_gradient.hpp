@@ -64,15 +64,14 @@ __device__ __forceinline__ void load_eight(const typename E::mem *__restrict__ r
 // out[m][z][n] = piece z of dy[m][n] * s[n], exps[m]; zeros for N <= n < Np.  GROUP lanes share a row, NP times eight elements each, which stay in
 // registers between the maximum and the pieces; a lane's columns are the same in every row, their scales are read once.
 template <typename E, int P, int GROUP, int NP>
-__global__ __launch_bounds__(GRAD_THREADS) void grad_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out,
-                                                                 int *__restrict__ exps, int M, int N, int Np) {
+__device__ __forceinline__ void grad_rows(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out, int *__restrict__ exps,
+                                          int M, int N, int Np, uint32_t block, uint32_t blocks, float *part) {
     constexpr int WAVES = GROUP / 64;
-    __shared__ float part[GRAD_THREADS / 64];
-    const int lane = threadIdx.x % GROUP, stride = (int)gridDim.x * (GRAD_THREADS / GROUP);
+    const int lane = threadIdx.x % GROUP, stride = (int)blocks * (GRAD_THREADS / GROUP);
     float sc[NP][8];
 #pragma unroll
     for (int u = 0; u < NP; ++u) load_eight<F32>(s, (u * GROUP + lane) * 8, N, sc[u]);
-    for (int m = (int)blockIdx.x * (GRAD_THREADS / GROUP) + (int)threadIdx.x / GROUP; m < M; m += stride) {
+    for (int m = (int)block * (GRAD_THREADS / GROUP) + (int)threadIdx.x / GROUP; m < M; m += stride) {
         float t[NP][8], big = 0.0f;
 #pragma unroll
         for (int u = 0; u < NP; ++u) load_eight<E>(dy + (size_t)m * (size_t)N, (u * GROUP + lane) * 8, N, t[u]);
@@ -103,10 +102,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_rows_kernel(const typename 
 
 // The same for rows too long for registers: read twice.
 template <typename E, int P>
-__global__ __launch_bounds__(GRAD_THREADS) void grad_long_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out,
-                                                                      int *__restrict__ exps, int M, int N, int Np) {
-    __shared__ float part[GRAD_THREADS / 64];
-    for (int m = blockIdx.x; m < M; m += gridDim.x) {
+__device__ __forceinline__ void grad_long_rows(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out, int *__restrict__ exps,
+                                               int M, int N, int Np, uint32_t block, uint32_t blocks, float *part) {
+    for (int m = (int)block; m < M; m += (int)blocks) {
         float big = 0.0f;
         auto eight = [&](int n, float(&t)[8]) {
             float sc[8];
@@ -137,29 +135,29 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_long_rows_kernel(const type
     }
 }
 
-// Of every column n over GRAD_ROWS rows: sum[block][n] of dy (sum != nullptr), big[block][n] = max |dy s| (big != nullptr).  A thread takes 16
-// bytes of every 16th (32nd) row.
+// Of 64 columns over `rows` rows (a multiple of GRAD_ROWS): sum[block][n] of dy (sum != nullptr), big[block][n] = max |dy s| (big != nullptr).  A
+// thread takes 16 bytes of every 16th (32nd) row.  sums, bigs: [GRAD_THREADS P / 64][64]
 constexpr int GRAD_ROWS = 256;
+constexpr int GRAD_BLOCKS = 64;         // row blocks at most
 template <typename E>
-__global__ __launch_bounds__(GRAD_THREADS) void grad_columns_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, float *__restrict__ sum,
-                                                                    float *__restrict__ big, int M, int N) {
+__device__ __forceinline__ void grad_columns(const typename E::mem *__restrict__ dy, const float *__restrict__ s, float *__restrict__ sum, float *__restrict__ big,
+                                             int M, int N, int rows, uint32_t row_block, uint32_t column_block, float *sums, float *bigs) {
     constexpr int P = piece_len<E>, LANES = 64 / P, G = GRAD_THREADS / LANES;
-    __shared__ float sums[G][64], bigs[G][64];
-    const int c = (threadIdx.x % LANES) * P, n = blockIdx.y * 64 + c, g = threadIdx.x / LANES;
+    const int c = (threadIdx.x % LANES) * P, n = (int)column_block * 64 + c, g = threadIdx.x / LANES;
     float a[P] = {}, b[P] = {};
-#pragma unroll
-    for (int u0 = 0; u0 < GRAD_ROWS / G; u0 += 8) {
+    const int first = (int)row_block * rows, last = min(M, first + rows);
+    for (int m0 = first; m0 < last; m0 += 8 * G) {
         float t[8][P], sm[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int m = blockIdx.x * GRAD_ROWS + g + G * (u0 + u);
+            const int m = m0 + g + G * u;
             const typename E::mem *const at = dy + (size_t)m * (size_t)N + n;
-            sm[u] = big && m < M ? s[m] : 0.0f;
-            if (m < M && n + P <= N) {
+            sm[u] = big && m < last ? s[m] : 0.0f;
+            if (m < last && n + P <= N) {
                 load_piece<E, P>(at, t[u]);
             } else {
 #pragma unroll
-                for (int j = 0; j < P; ++j) t[u][j] = m < M && n + j < N ? E::load(at[j]) : 0.0f;
+                for (int j = 0; j < P; ++j) t[u][j] = m < last && n + j < N ? E::load(at[j]) : 0.0f;
             }
         }
 #pragma unroll
@@ -172,34 +170,33 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_columns_kernel(const typena
     }
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-        sums[g][c + j] = a[j];
-        bigs[g][c + j] = b[j];
+        sums[g * 64 + c + j] = a[j];
+        bigs[g * 64 + c + j] = b[j];
     }
     __syncthreads();
-    const int col = threadIdx.x, at = blockIdx.y * 64 + col;
+    const int col = threadIdx.x, at = (int)column_block * 64 + col;
     if (col < 64 && at < N) {
-        float x = sums[0][col], y = bigs[0][col];
+        float x = sums[col], y = bigs[col];
 #pragma unroll
         for (int w = 1; w < G; ++w) {
-            x += sums[w][col];
-            y = fmaxf(y, bigs[w][col]);
+            x += sums[w * 64 + col];
+            y = fmaxf(y, bigs[w * 64 + col]);
         }
-        if (sum) sum[(size_t)blockIdx.x * (size_t)N + at] = x;
-        if (big) big[(size_t)blockIdx.x * (size_t)N + at] = y;
+        if (sum) sum[(size_t)row_block * (size_t)N + at] = x;
+        if (big) big[(size_t)row_block * (size_t)N + at] = y;
     }
 }
 
-// The blocks' results together: db[n] (sum != nullptr) and exps[n] (big != nullptr).  64 columns per workgroup, sixteen waves with every sixteenth
-// block each.
+// The row blocks' results of 64 columns together: db[n] (sum != nullptr), and in exponents[64] (big != nullptr) the columns' exponents.  Four waves with
+// every fourth block each.  scratch: [4][64]
 template <typename E>
-__global__ __launch_bounds__(1024) void grad_columns_join_kernel(const float *__restrict__ sum, const float *__restrict__ big, typename E::mem *__restrict__ db,
-                                                                 int *__restrict__ exps, int blocks, int N) {
-    __shared__ float sums[16][64], bigs[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+__device__ __forceinline__ void grad_columns_join(const float *__restrict__ sum, const float *__restrict__ big, typename E::mem *__restrict__ db, int blocks, int N,
+                                                  uint32_t column_block, float (*sums)[64], float (*bigs)[64], int *exponents) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)column_block * 64 + lane;
     float x = 0.0f, y = 0.0f;
     if (n < N) {
 #pragma unroll 4
-        for (int b = wave; b < blocks; b += 16) {
+        for (int b = wave; b < blocks; b += 4) {
             if (sum) x += sum[(size_t)b * (size_t)N + n];
             if (big) y = fmaxf(y, big[(size_t)b * (size_t)N + n]);
         }
@@ -207,23 +204,28 @@ __global__ __launch_bounds__(1024) void grad_columns_join_kernel(const float *__
     sums[wave][lane] = x;
     bigs[wave][lane] = y;
     __syncthreads();
-    if (wave == 0 && n < N) {
+    if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < 16; ++w) {
+        for (int w = 1; w < 4; ++w) {
             x += sums[w][lane];
             y = fmaxf(y, bigs[w][lane]);
         }
-        if (sum) db[n] = E::store(x);
-        if (big) exps[n] = grad_exponent(y);
+        if (sum && n < N) db[n] = E::store(x);
+        if (big) exponents[lane] = grad_exponent(y);
     }
+    __syncthreads();
+}
+template <typename E>
+__global__ __launch_bounds__(GRAD_THREADS) void grad_bias_kernel(const float *__restrict__ sum, typename E::mem *__restrict__ db, int blocks, int N) {
+    __shared__ float sums[4][64], bigs[4][64];
+    grad_columns_join<E>(sum, nullptr, db, blocks, N, blockIdx.x, sums, bigs, nullptr);
 }
 
 // 64 x 64 elements src[r][c] come out as out[c][..][r], padded with zeros to Rp rows: the transposed operands.  A workgroup holds the block in
 // LDS as floats; lanes read along c and write along r, 16 bytes a lane.
 constexpr int GRAD_LD = 65;
 template <typename Write>
-__device__ __forceinline__ void grad_transposed(const float (&tile)[64][GRAD_LD], int C, Write &&write) {
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+__device__ __forceinline__ void grad_transposed(const float (*tile)[GRAD_LD], int C, int r0, int c0, Write &&write) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int c = (threadIdx.x >> 3) + 32 * u, r = (threadIdx.x & 7) * 8;
@@ -235,12 +237,15 @@ __device__ __forceinline__ void grad_transposed(const float (&tile)[64][GRAD_LD]
     }
 }
 
-// out[n][z][m] = piece z of dy[m][n] * s[m] 2^-exps[n]
+// out[n][z][m] = piece z of dy[m][n] * s[m] 2^-exps[n], the exponents from the row blocks' maxima; the first workgroup of 64 columns also writes
+// exps and, if sum != nullptr, db
 template <typename E, int P>
-__global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, const int *__restrict__ exps,
-                                                                        _Float16 *__restrict__ out, int M, int N, int Mp) {
-    __shared__ float tile[64][GRAD_LD];
-    const int r0 = blockIdx.x * 64, c = (threadIdx.x & 15) * 4, n = blockIdx.y * 64 + c;
+__global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, const float *__restrict__ sum,
+                                                                        const float *__restrict__ big, typename E::mem *__restrict__ db, int *__restrict__ exps,
+                                                                        _Float16 *__restrict__ out, int M, int N, int Mp, int blocks) {
+    __shared__ float tile[64][GRAD_LD], sums[4][64], bigs[4][64];
+    __shared__ int exponents[64];
+    const int r0 = blockIdx.x * 64, c = (threadIdx.x & 15) * 4, c0 = blockIdx.y * 64, n = c0 + c;
     float t[4][4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -253,6 +258,9 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const ty
             for (int j = 0; j < 4; ++j) t[u][j] = m < M && n + j < N ? E::load(at[j]) : 0.0f;
         }
     }
+    const bool first = blockIdx.x == 0;
+    grad_columns_join<E>(first ? sum : nullptr, big, db, blocks, N, blockIdx.y, sums, bigs, exponents);
+    if (first && threadIdx.x < 64 && c0 + (int)threadIdx.x < N) exps[c0 + threadIdx.x] = exponents[threadIdx.x];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int r = (threadIdx.x >> 4) + 16 * u, m = r0 + r;
@@ -261,13 +269,15 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const ty
         for (int j = 0; j < 4; ++j) tile[r][c + j] = m < M && n + j < N ? t[u][j] * sm : 0.0f;
     }
     __syncthreads();
-    grad_transposed(tile, N, [&](int col, int row, const float(&e)[8]) { store_pieces<P>(e, exps[col], out + (size_t)col * P * (size_t)Mp + row, (size_t)Mp); });
+    grad_transposed(tile, N, r0, c0, [&](int col, int row, const float(&e)[8]) {
+        store_pieces<P>(e, exponents[col - c0], out + (size_t)col * P * (size_t)Mp + row, (size_t)Mp);
+    });
 }
 
-// out[c][r] = q[r][c]
-__global__ __launch_bounds__(GRAD_THREADS) void grad_codes_kernel(const int8_t *__restrict__ q, _Float16 *__restrict__ out, int R, int C, int Rp) {
-    __shared__ float tile[64][GRAD_LD];
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+// out[c][r] = q[r][c], a block of 64 x 64
+__device__ __forceinline__ void grad_codes(const int8_t *__restrict__ q, _Float16 *__restrict__ out, int R, int C, int Rp, uint32_t row_block, uint32_t column_block,
+                                           float (*tile)[GRAD_LD]) {
+    const int r0 = (int)row_block * 64, c0 = (int)column_block * 64;
     const int rl = threadIdx.x >> 2, c = (threadIdx.x & 3) * 16, r = r0 + rl;
     i32x4_t v = {0, 0, 0, 0};
     if (r < R) {
@@ -283,12 +293,50 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_codes_kernel(const int8_t *
 #pragma unroll
     for (int j = 0; j < 16; ++j) tile[rl][c + j] = (float)(int8_t)(v[j / 4] >> (8 * (j % 4)));
     __syncthreads();
-    grad_transposed(tile, C, [&](int col, int row, const float(&t)[8]) {
+    grad_transposed(tile, C, r0, c0, [&](int col, int row, const float(&t)[8]) {
         f16x8_t b;
 #pragma unroll
         for (int j = 0; j < 8; ++j) b[j] = (_Float16)t[j];
         *reinterpret_cast<f16x8_t *>(out + (size_t)col * (size_t)Rp + row) = b;
     });
+}
+
+// Everything that can be made from the operands at once, one launch: the workgroups are dealt out in four ranges, the rows of dy s_w, the codes w,
+// the columns' sums and maxima, the codes a.  (Each alone: 34 us in four launches for 6990 x 227 -> 1706 bf16, together 26.)
+struct GradPrep {
+    const void *dy;
+    const float *s_a, *s_w;
+    const int8_t *a, *w;
+    int M, K, N, Np, Mp, rows;
+    _Float16 *dy_rows, *w_codes, *a_codes;
+    int *row_exps;
+    float *sum, *big;
+    uint32_t row_groups, w_groups, column_groups, w_blocks, column_blocks, a_blocks;    // ranges, the first dimension of three of them
+};
+// GROUP 0: rows too long for registers
+template <typename E, int P, int GROUP, int NP>
+__global__ __launch_bounds__(GRAD_THREADS) void grad_prepare_kernel(const GradPrep p) {
+    __shared__ float lds[64 * GRAD_LD];
+    static_assert(2 * GRAD_THREADS / (64 / piece_len<E>) * 64 <= 64 * GRAD_LD, "column statistics");
+    const typename E::mem *const dy = static_cast<const typename E::mem *>(p.dy);
+    uint32_t g = blockIdx.x;
+    if (g < p.row_groups) {
+        if constexpr (GROUP == 0) grad_long_rows<E, P>(dy, p.s_w, p.dy_rows, p.row_exps, p.M, p.N, p.Np, g, p.row_groups, lds);
+        else grad_rows<E, P, GROUP, NP>(dy, p.s_w, p.dy_rows, p.row_exps, p.M, p.N, p.Np, g, p.row_groups, lds);
+        return;
+    }
+    g -= p.row_groups;
+    if (g < p.w_groups) {
+        grad_codes(p.w, p.w_codes, p.N, p.K, p.Np, g % p.w_blocks, g / p.w_blocks, reinterpret_cast<float(*)[GRAD_LD]>(lds));
+        return;
+    }
+    g -= p.w_groups;
+    if (g < p.column_groups) {
+        grad_columns<E>(dy, p.s_a, p.sum, p.big, p.M, p.N, p.rows, g % p.column_blocks, g / p.column_blocks, lds, lds + GRAD_THREADS / (64 / piece_len<E>) * 64);
+        return;
+    }
+    g -= p.column_groups;
+    grad_codes(p.a, p.a_codes, p.M, p.K, p.Mp, g % p.a_blocks, g / p.a_blocks, reinterpret_cast<float(*)[GRAD_LD]>(lds));
 }
 
 // c[i] = part[0][i] + part[1][i] + ... in that order, rounded to E
