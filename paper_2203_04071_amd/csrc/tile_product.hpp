@@ -92,7 +92,7 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_i, uint32_t 
 // 128 x 64 would read 1.5 times as much) and leave 512 registers a lane, half of them sums.
 //
 // DMA: rows are multiples of 16 bytes and 16-byte aligned; pieces go from memory to LDS without registers, requested NB - 1 stages ahead, one
-// barrier a stage.  8192 x 8192 x 8192 int8 -> bf16 480 us, 2.3 POP/s; on all compute units the clock falls to 1.8 GHz, at which the matrix
+// barrier a stage.  8192 x 8192 x 8192 int8 -> bf16 466 - 478 us, 2.3 POP/s; on all compute units the clock falls to 1.8 GHz, at which the matrix
 // pipe is busy for 3/4 of the time (alone on the chip a workgroup keeps it busy for 83 %).
 // Otherwise (rows of any length and address): pieces pass through registers, three stages ahead, which also put zeros behind a row's end.  Bounded by
 // the memory pipe, which takes longer over 16 bytes at an odd address: 1111 x 4096 -> 999 21 us against 14, 4095 26 us.
