@@ -14,6 +14,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 constexpr int INT8_MAX_K = 131071;              // (-128)^2 K < 2^31
 constexpr long long MAX_TILES = 1ll << 24;      // a launch is limited to 2^32 threads
+constexpr int TOKENS_GROUPS = 1 << 23;         // the same for workgroups of 512
 constexpr int GRAD_MAX = 2097152;               // 256 rows of its pieces (6 bytes an element) are addressed with 32 bits
 
 int int8_args(const char *who, int M, int K, int N, int type) {
@@ -68,6 +69,7 @@ bool long_ragged(const adapt::TileParams &p) {
 // 9.1 against 17, 8 x 4096 -> 16384 17 against 12.6.  Rows that are no multiple of 16 bytes (up to 64 tokens): always.
 int tokens_kernel_mt(int M, int N, bool dma) {
     const long long n16 = ((long long)N + 15) / 16;
+    if (n16 >= TOKENS_GROUPS) return 0;
     const int mts[3] = {1, 2, 4};
     int best = 0;
     long long best_cost = 0;
@@ -107,7 +109,7 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
     p.c = q.y;
     const TilePlan small = one_tile(p.I, p.J, p.Kb, 64, 64);
     if (q.act == 2) {       // (tanh: one kernel for each way of reading)
-        if (q.M <= 16) launch_tokens<E, 1, true>(q, s);
+        if (q.M <= 16 && q.N <= 16 * (TOKENS_GROUPS - 1)) launch_tokens<E, 1, true>(q, s);
         else if (dma) launch_tile<adapt::TileI8, E, 64, 64, 128, 4, true, true>(p, small, s);
         else launch_tile<adapt::TileI8, E, 64, 64, 64, 2, false, true>(p, small, s);
         return;

@@ -130,8 +130,9 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
         }
     }
 
-    // requests: number q of a wave covers rows 8 (4 q + wave) .. + 7 of the tile, lane l row l / 8, piece (l % 8) ^ (row % 8)
-    auto swizzle = [](int row) { return SB == 256 ? row & 15 : SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
+    // requests: number q of a wave covers RQ rows from RQ (4 q + wave) on, lane l row l / PIECES and the piece that belongs at place l % PIECES
+    static_assert(SB == 64 || SB == 128, "places of a row's pieces");
+    auto swizzle = [](int row) { return SB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
     const int prow = lane / PIECES, piece16 = ((lane % PIECES) ^ swizzle(RQ * wave + prow)) * 16;
     const char *abase = p.a + (size_t)i0 * p.lda + k0, *bbase = p.b + (size_t)j0 * p.ldb;
     uint32_t voff[NQ];

@@ -299,6 +299,25 @@ def test_int8_linear_backward_rows_of_very_different_elements(B, name):
     within(dw, ww, mw, M, name, KEPT[name], far_below((dy * s_a[:, None]).T, a))
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("exponent", [-20, -27, -31, -36])
+def test_int8_linear_backward_elements_far_below_their_rows_largest(B, name, exponent):
+    """What is 2^20 to 2^36 times smaller than the largest element, which meets nothing but zeros, is not lost."""
+    rng = np.random.default_rng(-exponent)
+    M, K, N = 96, 40, 130
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    dy = np.ldexp(rng.uniform(0.5, 1.0, (M, N)), exponent)
+    dy[:, 17], dy[23, :] = 1.0, 1.0
+    w[17], a[23] = 0, 0
+    dy, dyd = (lambda t: (t.float().numpy(), t.cuda()))(rounded(dy.astype(np.float32), name))
+    dx, dw, _ = B.adapt_int8_linear_backward(dyd, dev(a), dev(s_a), dev(w), dev(s_w))
+    (wx, mx), (ww, mw), _ = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+    rows, cols = np.arange(M) != 23, np.arange(N) != 17
+    assert np.abs(wx[rows]).max() > 0 and np.abs(ww[cols]).max() > 0
+    within(dx[dev(rows)], wx[rows], mx[rows], N, name, KEPT[name], far_below(dy * s_w, w)[rows])
+    within(dw[dev(cols)], ww[cols], mw[cols], M, name, KEPT[name], far_below((dy * s_a[:, None]).T, a)[cols])
+
+
 @pytest.mark.parametrize("M,K,N", [(5, 40, 9000), (9000, 40, 5), (70, 33, 2100), (2100, 33, 70), (66, 20, 1100), (300, 16, 4500), (3, 5, 600)])
 def test_int8_linear_backward_long_sums(B, M, K, N):
     rng = np.random.default_rng(M)
@@ -611,6 +630,18 @@ def test_int8_linear_beyond_32_bits(B, big, K):
     y = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), dtype=torch.bfloat16)
     for rows in (slice(0, 2), slice(65070, 65080), slice(M - 5, M)):
         same_bits(y[rows], rounded(ot.int8_linear(a[rows], s_a[rows], w, s_w), "bf16"))
+
+
+@pytest.mark.parametrize("act", [0, 2])
+def test_int8_linear_more_channels_than_a_launch_has_threads(B, big, act):
+    torch = big
+    N, K = (1 << 27) + 37, 17
+    w = torch.randint(-128, 128, (N, K), dtype=torch.int8, device="cuda")
+    a, s_a, s_w = codes(np.random.default_rng(1), 1, K), np.array([0.01], np.float32), torch.full((N,), 0.01, device="cuda")
+    y = B.adapt_int8_linear(dev(a), dev(s_a), w, s_w, act=act)
+    for at in (slice(0, 100), slice(N - 100, N)):
+        want = ot.int8_linear(a, s_a, w[at].cpu().numpy(), np.full(100, 0.01, np.float32), None, act, tanh=orc.tanh)
+        same_bits(y[:, at], rounded(want, "f32"))
 
 
 def test_int8_linear_backward_beyond_32_bits(B, big):
