@@ -23,25 +23,40 @@ int int8_args(const char *who, int M, int K, int N, int type) {
     return ADAPT_OK;
 }
 
-template <class Op, class E, int TM, int TN, int SB, int NB, bool DMA, bool TANH = false>
-void launch_tile(adapt::TileParams p, const TilePlan &t, hipStream_t s) {
+int grad_limits(const char *who, int M, int K, int N) {
+    if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
+    // (three matrices in blocks of 64 x 64, a workgroup of 256 each, in one launch of less than 2^32 threads)
+    if ((long long)M * K >> 34 || (long long)N * K >> 34 || (long long)M * N >> 34) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a matrix of 2^34 elements or more", who);
+    return ADAPT_OK;
+}
+
+void set_tiles(adapt::TileParams &p, const TilePlan &t, size_t element) {
     p.tiles_i = (int)t.tiles_i;
     p.tiles_j = (int)t.tiles_j;
     p.Kb_split = (int)t.kb_split;
-    p.stream = (double)p.I * (double)p.J * sizeof(typename E::mem) > 32.0e6;
-    adapt::tile_product_kernel<Op, E, TM, TN, SB, NB, DMA, TANH><<<dim3((unsigned)(t.tiles_i * t.tiles_j), (unsigned)t.split), adapt::TILE_THREADS, 0, s>>>(p);
+    p.stream = (double)p.I * (double)p.J * (double)element > 32.0e6;
 }
 
-// whole stages go from memory to LDS by themselves: rows of 16-byte pieces
-template <class Op, class E>
-void launch_tiles(const adapt::TileParams &p, const TilePlan &t, hipStream_t s) {
-    switch (t.kind) {
-        case TILE_256x256: launch_tile<Op, E, 256, 256, 64, 4, true>(p, t, s); break;
-        case TILE_256x128: launch_tile<Op, E, 256, 128, 128, 3, true>(p, t, s); break;
-        case TILE_128x128: launch_tile<Op, E, 128, 128, 128, 4, true>(p, t, s); break;
-        case TILE_128x128_TWO: launch_tile<Op, E, 128, 128, 64, 3, true>(p, t, s); break;
-        case TILE_128x64: launch_tile<Op, E, 128, 64, 128, 4, true>(p, t, s); break;
-        default: launch_tile<Op, E, 64, 64, 128, 4, true>(p, t, s); break;
+template <class E, int TM, int TN, int SB, int NB, bool DMA, bool TANH = false>
+void launch_tile(adapt::TileParams p, const TilePlan &t, hipStream_t s) {
+    set_tiles(p, t, sizeof(typename E::mem));
+    adapt::tile_product_kernel<adapt::TileI8, E, TM, TN, SB, NB, DMA, TANH><<<(unsigned)(t.tiles_i * t.tiles_j), adapt::TILE_THREADS, 0, s>>>(p);
+}
+template <class E, int TM, int TN, int SB, int NB, bool DMA>
+void launch_tile(const adapt::TilePair &p, unsigned groups, hipStream_t s) {
+    adapt::tile_product_kernel<adapt::TileF16, E, TM, TN, SB, NB, DMA><<<groups, adapt::TILE_THREADS, 0, s>>>(p);
+}
+
+// whole stages go from memory to LDS by themselves: rows of 16-byte pieces.  `t`: a plan, or the number of workgroups
+template <class E, class Params, class Tiles>
+void launch_tiles(TileKind kind, const Params &p, const Tiles &t, hipStream_t s) {
+    switch (kind) {
+        case TILE_256x256: launch_tile<E, 256, 256, 64, 4, true>(p, t, s); break;
+        case TILE_256x128: launch_tile<E, 256, 128, 128, 3, true>(p, t, s); break;
+        case TILE_128x128: launch_tile<E, 128, 128, 128, 4, true>(p, t, s); break;
+        case TILE_128x128_TWO: launch_tile<E, 128, 128, 64, 3, true>(p, t, s); break;
+        case TILE_128x64: launch_tile<E, 128, 64, 128, 4, true>(p, t, s); break;
+        default: launch_tile<E, 64, 64, 128, 4, true>(p, t, s); break;
     }
 }
 
@@ -110,8 +125,8 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
     const TilePlan small = one_tile(p.I, p.J, p.Kb, 64, 64);
     if (q.act == 2) {       // (tanh: one kernel for each way of reading)
         if (q.M <= 16 && q.N <= 16 * (TOKENS_GROUPS - 1)) launch_tokens<E, 1, true>(q, s);
-        else if (dma) launch_tile<adapt::TileI8, E, 64, 64, 128, 4, true, true>(p, small, s);
-        else launch_tile<adapt::TileI8, E, 64, 64, 64, 2, false, true>(p, small, s);
+        else if (dma) launch_tile<E, 64, 64, 128, 4, true, true>(p, small, s);
+        else launch_tile<E, 64, 64, 64, 2, false, true>(p, small, s);
         return;
     }
     switch (tokens_kernel_mt(q.M, q.N, dma)) {
@@ -119,10 +134,14 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
         case 2: launch_tokens<E, 2>(q, s); return;
         case 4: launch_tokens<E, 4>(q, s); return;
     }
-    if (dma) launch_tiles<adapt::TileI8, E>(p, tile_plan(p.I, p.J, p.Kb, device_cus(), 1), s);
-    else if (long_ragged(p)) launch_tile<adapt::TileI8, E, 128, 64, 128, 2, false>(p, one_tile(p.I, p.J, p.Kb, 128, 64), s);
-    else launch_tile<adapt::TileI8, E, 64, 64, 64, 2, false>(p, small, s);
+    if (dma) {
+        const TilePlan t = tile_plan(p.I, p.J, p.Kb, device_cus(), 1);
+        launch_tiles<E>(t.kind, p, t, s);
+    } else if (long_ragged(p)) launch_tile<E, 128, 64, 128, 2, false>(p, one_tile(p.I, p.J, p.Kb, 128, 64), s);
+    else launch_tile<E, 64, 64, 64, 2, false>(p, small, s);
 }
+
+int grad_whole(long long R) { return (int)((R + adapt::GRAD_STAGE - 1) / adapt::GRAD_STAGE * adapt::GRAD_STAGE); }
 
 // Workspace of one gradient c [I][J], the sums over R: rows of the pieces of dy s [I], rows of codes [J], the rows' exponents, partial sums of
 // a split product.
@@ -132,12 +151,13 @@ struct GradPlan {
     TilePlan tile;
     size_t b, exps, part, bytes;    // offsets (a at 0)
 };
-GradPlan grad_plan(long long I, long long J, long long R, int P) {
+// (the tile comes from grad_plans)
+GradPlan grad_plan(long long I, long long J, long long R, int P, const TilePlan &tile) {
     GradPlan g{};
-    g.Rp = (int)((R + adapt::GRAD_STAGE - 1) / adapt::GRAD_STAGE * adapt::GRAD_STAGE);
+    g.Rp = grad_whole(R);
     g.row = 2ll * P * g.Rp;
     g.row_b = 2ll * g.Rp;
-    g.tile = tile_plan(I, J, g.row, device_cus(), 8);
+    g.tile = tile;
     g.b = round256((size_t)I * (size_t)g.row);
     g.exps = g.b + round256((size_t)J * (size_t)g.row_b);
     g.part = g.exps + round256((size_t)I * 4);
@@ -154,8 +174,32 @@ int column_rows(int M) {
 int column_blocks(int M) { return (int)((M + (long long)column_rows(M) - 1) / column_rows(M)); }
 size_t column_bytes(int M, int N) { return 2 * round256((size_t)(M ? column_blocks(M) : 1) * (size_t)N * 4); }
 
-template <class E>
-void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_t s) {
+// Workspace of a call: what dx needs, what dw needs, the columns' partial results.
+struct GradPlans {
+    GradPlan x, w;              // all zeros where the gradient is not wanted
+    bool joint;                 // their products are one launch
+    int first;                  // 1: dw's workgroups come first
+    size_t bytes;
+};
+GradPlans grad_plans(int M, int K, int N, int type, bool want_dx, bool want_dw) {
+    const int P = grad_pieces(type), cus = device_cus();
+    const long long I[2] = {M, N}, J[2] = {K, K}, Kb[2] = {2ll * P * grad_whole(N), 2ll * P * grad_whole(M)};
+    // (a gradient has the same bits whatever else is asked for: the number of parts is the pair's, the tile that which is best for it alone)
+    TilePairPlan t = tile_pair_plan(I, J, Kb, cus);
+    if (!want_dx || !want_dw) {
+        t.joint = false;
+        for (int x = 0; x < 2; ++x) t.plan[x] = tile_plan(I[x], J[x], Kb[x], cus, t.plan[x].split);
+    }
+    GradPlans g{};
+    if (want_dx) g.x = grad_plan(M, K, N, P, t.plan[0]);
+    if (want_dw) g.w = grad_plan(N, K, M, P, t.plan[1]);
+    g.joint = t.joint;
+    g.first = t.first;
+    g.bytes = g.x.bytes + g.w.bytes + column_bytes(M, N);
+    return g;
+}
+
+adapt::TileParams grad_params(const GradPlan &g, char *ws, int I, int J, void *c, size_t element) {
     adapt::TileParams p{};
     p.a = ws;
     p.b = ws + g.b;
@@ -166,16 +210,18 @@ void grad_product(const GradPlan &g, char *ws, int I, int J, void *c, hipStream_
     p.Kb_b = (int)g.row_b;
     p.lda = (uint32_t)g.row;
     p.ldb = (uint32_t)g.row_b;
-    if (g.tile.split == 1) {
-        p.c = c;
-        launch_tiles<adapt::TileF16, E>(p, g.tile, s);
-    } else {
-        float *const part = reinterpret_cast<float *>(ws + g.part);
-        const size_t n = (size_t)I * (size_t)J;
-        p.c = part;
-        launch_tiles<adapt::TileF16, adapt::F32>(p, g.tile, s);
-        adapt::grad_join_kernel<E><<<ew_grid(n / 4 + 1), 256, 0, s>>>(part, g.tile.split, n, static_cast<typename E::mem *>(c));
-    }
+    p.parts = g.tile.split > 1;
+    p.c = p.parts ? ws + g.part : c;
+    set_tiles(p, g.tile, p.parts ? 4 : element);
+    return p;
+}
+unsigned grad_groups(const GradPlan &g) { return (unsigned)(g.tile.tiles_i * g.tile.tiles_j * g.tile.split); }
+
+template <class E>
+void grad_join(const GradPlan &g, const char *ws, int I, int J, void *c, hipStream_t s) {
+    if (g.tile.split == 1) return;
+    const size_t n = (size_t)I * (size_t)J;
+    adapt::grad_join_kernel<E><<<ew_grid(n / 4 + 1), 256, 0, s>>>(reinterpret_cast<const float *>(ws + g.part), g.tile.split, n, static_cast<typename E::mem *>(c));
 }
 
 // a wave per row up to 1024 elements, a workgroup up to 8192 (quantize_tokens has the like); a workgroup takes several rows, whose scales of the
@@ -191,12 +237,11 @@ void prepare(const adapt::GradPrep &p, unsigned groups, hipStream_t s) {
     else adapt::grad_prepare_kernel<E, P, 0, 0><<<groups, T, 0, s>>>(p);
 }
 
-// Workspace: what dx needs, what dw needs, the columns' partial results.
 template <class E, int P>
-void gradients(const adapt::Int8Params &q, const void *dy, void *dx, void *dw, void *db_dev, char *ws, hipStream_t s) {
+void gradients(const adapt::Int8Params &q, const GradPlans &plans, const void *dy, void *dx, void *dw, void *db_dev, char *ws, hipStream_t s) {
     typedef typename E::mem mem;
     mem *const db = static_cast<mem *>(db_dev);
-    const GradPlan gx = dx ? grad_plan(q.M, q.K, q.N, P) : GradPlan{}, gw = dw ? grad_plan(q.N, q.K, q.M, P) : GradPlan{};
+    const GradPlan &gx = plans.x, &gw = plans.w;
     char *const wx = ws, *const ww = ws + gx.bytes, *const wc = ww + gw.bytes;
     auto blocks = [](int n) { return (uint32_t)((n + 63) / 64); };
     adapt::GradPrep p{};
@@ -234,7 +279,11 @@ void gradients(const adapt::Int8Params &q, const void *dy, void *dx, void *dw, v
     }
     const uint32_t groups = p.row_groups + p.w_groups + p.column_groups + a_groups;
     if (groups) prepare<E, P>(p, groups, s);
-    if (dx) grad_product<E>(gx, wx, q.M, q.K, dx, s);
+    adapt::TileParams px{}, pw{};
+    if (dx) px = grad_params(gx, wx, q.M, q.K, dx, sizeof(mem));
+    if (dw) pw = grad_params(gw, ww, q.N, q.K, dw, sizeof(mem));
+    const unsigned nx = grad_groups(gx), nw = grad_groups(gw);
+    if (dx && !plans.joint) launch_tiles<E>(gx.tile.kind, adapt::TilePair{{px, px}, nx}, nx, s);
     if (dw && gw.Rp) {
         adapt::grad_turned_rows_kernel<E, P><<<dim3((unsigned)gw.Rp / 64, blocks(q.N)), 256, 0, s>>>(
             static_cast<const mem *>(dy), q.s_a, p.sum, p.big, db, reinterpret_cast<int *>(ww + gw.exps), reinterpret_cast<_Float16 *>(ww), q.M, q.N, gw.Rp,
@@ -243,7 +292,10 @@ void gradients(const adapt::Int8Params &q, const void *dy, void *dx, void *dw, v
         if (dw) adapt::fill_u32_kernel<<<ew_grid((size_t)q.N), 256, 0, s>>>(reinterpret_cast<uint32_t *>(ww + gw.exps), 0u, (size_t)q.N);
         if (db) adapt::grad_bias_kernel<E><<<blocks(q.N), adapt::GRAD_THREADS, 0, s>>>(p.sum, db, column_blocks(q.M), q.N);
     }
-    if (dw) grad_product<E>(gw, ww, q.N, q.K, dw, s);
+    if (plans.joint) launch_tiles<E>(gx.tile.kind, plans.first ? adapt::TilePair{{pw, px}, nw} : adapt::TilePair{{px, pw}, nx}, nx + nw, s);
+    else if (dw) launch_tiles<E>(gw.tile.kind, adapt::TilePair{{pw, pw}, nw}, nw, s);
+    if (dx) grad_join<E>(gx, wx, q.M, q.K, dx, s);
+    if (dw) grad_join<E>(gw, ww, q.N, q.K, dw, s);
 }
 
 }  // namespace
@@ -274,14 +326,8 @@ int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want
     if (!bytes) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: bytes is NULL", who);
     *bytes = 0;
     if (int rc = int8_args(who, M, K, N, type)) return rc;
-    const int P = grad_pieces(type);
-    if (M > GRAD_MAX || K > GRAD_MAX || N > GRAD_MAX) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a size above %d", who, GRAD_MAX);
-    // (three matrices in blocks of 64 x 64, a workgroup of 256 each, in one launch of less than 2^32 threads)
-    if ((long long)M * K >> 34 || (long long)N * K >> 34 || (long long)M * N >> 34) return fail(ADAPT_ERR_UNSUPPORTED, "%s: a matrix of 2^34 elements or more", who);
-    size_t need = column_bytes(M, N);
-    if (want_dw && N && K) need += grad_plan(N, K, M, P).bytes;
-    if (want_dx && M && K) need += grad_plan(M, K, N, P).bytes;
-    *bytes = need;
+    if (int rc = grad_limits(who, M, K, N)) return rc;
+    *bytes = grad_plans(M, K, N, type, want_dx && M && K, want_dw && N && K).bytes;
     return ADAPT_OK;
 }
 
@@ -301,17 +347,18 @@ int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev
     for (const void *g : {(const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
         if (g && (g == dy_dev || g == (const void *)a_dev || g == (const void *)w_dev))
             return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
-    size_t need = 0;
-    if (int rc = adapt_int8_linear_backward_workspace(M, K, N, type, want_dx, want_dw, &need)) return rc;
+    if (int rc = grad_limits(who, M, K, N)) return rc;
+    const GradPlans plans = grad_plans(M, K, N, type, want_dx, want_dw);
+    const size_t need = plans.bytes;
     if (need && (!workspace_dev || workspace_bytes < need || off_by(workspace_dev, 256)))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, need);
     const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, nullptr, nullptr, M, K, N, 0};
     char *const ws = static_cast<char *>(workspace_dev);
     void *const dx = want_dx ? dx_dev : nullptr, *const dw = want_dw ? dw_dev : nullptr, *const db = want_db ? db_dev : nullptr;
     hipStream_t s = (hipStream_t)stream;
-    if (type == ADAPT_F32) gradients<adapt::F32, 2>(p, dy_dev, dx, dw, db, ws, s);
-    else if (type == ADAPT_F16) gradients<adapt::F16, 2>(p, dy_dev, dx, dw, db, ws, s);
-    else gradients<adapt::BF16, 1>(p, dy_dev, dx, dw, db, ws, s);
+    if (type == ADAPT_F32) gradients<adapt::F32, 2>(p, plans, dy_dev, dx, dw, db, ws, s);
+    else if (type == ADAPT_F16) gradients<adapt::F16, 2>(p, plans, dy_dev, dx, dw, db, ws, s);
+    else gradients<adapt::BF16, 1>(p, plans, dy_dev, dx, dw, db, ws, s);
     HIP_TRY(hipGetLastError());
     return ADAPT_OK;
 }

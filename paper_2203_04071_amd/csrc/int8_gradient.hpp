@@ -347,6 +347,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict_
         if (i + 4 <= n) {
             float s[4], t[4];
             load_piece<F32, 4>(part + i, s);
+#pragma unroll 8
             for (int z = 1; z < parts; ++z) {
                 load_piece<F32, 4>(part + (size_t)z * n + i, t);
 #pragma unroll

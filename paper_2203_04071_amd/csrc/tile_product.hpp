@@ -26,18 +26,27 @@ struct TileParams {
     // int8: rescaling by row and column, bias, activation
     const float *s_i, *s_j, *bias;
     int act;
-    int Kb_split;               // bytes of a row that a workgroup sums over: blockIdx.y takes the ones from y Kb_split, into c + y I J
+    int Kb_split;               // fp16: bytes of a row that a workgroup sums over: number y takes the ones from y Kb_split, into c + y I J
+    bool parts;                 // fp16: c is fp32 whatever E, sums of parts
     int stream;                 // c is larger than the caches: written past them
     void *c;                    // [I][J]
 };
 
+// One product, or two of fp16 numbers (a layer's two gradients) in one launch.
+struct TilePair {
+    TileParams p[2];
+    uint32_t first;             // workgroups of the first one
+};
+
 struct TileI8 {
     typedef i32x16_t acc_t;
+    typedef TileParams args_t;
     static constexpr bool INT = true;
     static __device__ __forceinline__ acc_t mfma(i32x4_t a, i32x4_t b, acc_t c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
 struct TileF16 {
     typedef tile_f32x16_t acc_t;
+    typedef TilePair args_t;
     static constexpr bool INT = false;
     static __device__ __forceinline__ acc_t mfma(i32x4_t a, i32x4_t b, acc_t c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
@@ -74,6 +83,11 @@ __device__ __forceinline__ i32x4_t row_piece(const char *__restrict__ row, int k
     return v;
 }
 
+__device__ __forceinline__ bool tile_second(const TileParams &) { return false; }
+__device__ __forceinline__ bool tile_second(const TilePair &a) { return blockIdx.x >= a.first; }
+__device__ __forceinline__ const TileParams &tile_params(const TileParams &a, bool) { return a; }
+__device__ __forceinline__ const TileParams &tile_params(const TilePair &a, bool second) { return a.p[second]; }
+
 // Which tile a workgroup computes.  Consecutive workgroups go to different XCDs, each with an L2 of its own: an XCD gets a contiguous
 // range of tiles, and the range runs through groups of four rows of tiles, so that the tiles in flight on an XCD share operands.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_i, uint32_t tiles_j, uint32_t &ti, uint32_t &tj) {
@@ -82,6 +96,82 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_i, uint32_t 
     const uint32_t group = 4 * tiles_j, g = t / group, first = g * 4, rows = min(4u, tiles_i - first), in = t - g * group;
     ti = first + in % rows;
     tj = in / rows;
+}
+
+// columns of a wave's outputs that turn through LDS at a time
+template <class E, int WJ>
+constexpr int turn_columns = WJ * (int)sizeof(typename E::mem) < 256 ? WJ : 256 / (int)sizeof(typename E::mem);
+template <class E, int TM, int TN>
+constexpr int turn_bytes = 2 * TM * (turn_columns<E, TN / 2> * (int)sizeof(typename E::mem) + 16);
+constexpr int tile_larger(int a, int b) { return a > b ? a : b; }
+
+// Register v of lane l holds column 8 (v / 4) + 4 (l / 32) + v % 4 of row l % 32 of a 32 x 32 block.  A wave turns its outputs through
+// LDS, up to 256 bytes of every row at a time, so that a store is 16 bytes of a lane and a row's pieces lie together.
+template <class Op, class E, int TM, int TN, bool TANH, int LDS_BYTES>
+__device__ __forceinline__ void tile_output(const TileParams &p, const typename Op::acc_t (&acc)[TM / 64][TN / 64], char *lds, const float *side, int i0, int j0, uint32_t part) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wi = (wave & 1) * (TM / 2), wj = (wave >> 1) * (TN / 2);
+    constexpr int BI = TM / 64, BJ = TN / 64, WI = TM / 2, WJ = TN / 2, SIZE = (int)sizeof(typename E::mem);
+    constexpr int CB = turn_columns<E, WJ>;                        // columns at a time
+    constexpr int ROW = CB * SIZE + 16;                            // (rows start in different banks)
+    constexpr int PL = piece_len<E>, LANES = CB / PL;              // lanes that store a row
+    static_assert(4 * WI * ROW <= LDS_BYTES, "the turned outputs of four waves");
+    char *const turn = lds + wave * (WI * ROW);
+    typename E::mem *const c = static_cast<typename E::mem *>(p.c) + (size_t)part * (size_t)p.I * (size_t)p.J;
+    const float floor = int8_floor(p.act);
+    const bool whole = i0 + TM <= p.I && j0 + TN <= p.J;
+#pragma unroll
+    for (int cb = 0; cb < WJ / CB; ++cb) {
+#pragma unroll
+        for (int bi = 0; bi < BI; ++bi) {
+            const float s_i = side[wi + 32 * bi + (lane & 31)];
+#pragma unroll
+            for (int bj = cb * (CB / 32); bj < (cb + 1) * (CB / 32); ++bj) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int col = 32 * bj + 8 * g + 4 * (lane >> 5);
+                    float y[4];
+                    if constexpr (Op::INT) {
+                        const tile_f32x4_t sv = *reinterpret_cast<const tile_f32x4_t *>(&side[TM + wj + col]);
+                        const tile_f32x4_t bv = *reinterpret_cast<const tile_f32x4_t *>(&side[TM + TN + wj + col]);
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) y[v] = int8_finish<TANH>(acc[bi][bj][4 * g + v], s_i, sv[v], bv[v], floor, p.act);
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) y[v] = __builtin_amdgcn_ldexpf(acc[bi][bj][4 * g + v], __float_as_int(s_i));
+                    }
+                    typedef typename E::mem quad_t __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<quad_t *>(turn + (32 * bi + (lane & 31)) * ROW + (col - cb * CB) * SIZE) =
+                        quad_t{E::store(y[0]), E::store(y[1]), E::store(y[2]), E::store(y[3])};
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");       // (a wave's own outputs: no barrier)
+        const int r0 = lane / LANES, col = (lane % LANES) * PL, j = j0 + wj + cb * CB + col;
+        const char *from = turn + r0 * ROW + col * SIZE;
+        typename E::mem *to = c + (size_t)(i0 + wi + r0) * (size_t)p.J + (size_t)j;
+        const size_t next = (size_t)(64 / LANES) * (size_t)p.J;
+        typedef i32x4_t piece_t __attribute__((aligned(2)));       // (a row starts at any element)
+        if (whole && p.stream) {        // (outputs beyond the caches: 6400 x 512 -> 2048 fp32 20.0 -> 18.2 us)
+#pragma unroll 8
+            for (int u = 0; u < WI * LANES / 64; ++u, from += 64 / LANES * ROW, to += next)
+                __builtin_nontemporal_store(*reinterpret_cast<const i32x4_t *>(from), reinterpret_cast<piece_t *>(to));
+        } else if (whole) {
+#pragma unroll 8
+            for (int u = 0; u < WI * LANES / 64; ++u, from += 64 / LANES * ROW, to += next) *reinterpret_cast<piece_t *>(to) = *reinterpret_cast<const i32x4_t *>(from);
+        } else {
+#pragma unroll 1
+            for (int i = i0 + wi + r0; i < min(p.I, i0 + wi + WI); i += 64 / LANES, from += 64 / LANES * ROW, to += next) {
+                if (j + PL <= p.J) {
+                    *reinterpret_cast<piece_t *>(to) = *reinterpret_cast<const i32x4_t *>(from);
+                } else {
+#pragma unroll 1
+                    for (int x = 0; j + x < p.J; ++x) to[x] = reinterpret_cast<const typename E::mem *>(from)[x];
+                }
+            }
+        }
+        if (cb + 1 < WJ / CB) asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    }
 }
 
 // TM x TN outputs per workgroup, (TM / 2) x (TN / 2) per wave in blocks of 32 x 32; NB LDS buffers (stages) of SB bytes of every row.  A row's pieces
@@ -97,21 +187,29 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_i, uint32_t 
 // Otherwise (rows of any length and address): pieces pass through registers, three stages ahead, which also put zeros behind a row's end.  Bounded by
 // the memory pipe, which takes longer over 16 bytes at an odd address: 1111 x 4096 -> 999 21 us against 14, 4095 26 us.
 template <class Op, class E, int TM, int TN, int SB, int NB, bool DMA, bool TANH = false>
-__global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TileParams p) {
-    const int k0 = (int)blockIdx.y * p.Kb_split, Kb = min(p.Kb - k0, p.Kb_split);
+__global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const typename Op::args_t args) {
+    const bool second = tile_second(args);
+    const TileParams &p = tile_params(args, second);
+    uint32_t id = blockIdx.x, part = 0;
+    if constexpr (!Op::INT) {
+        if (second) id -= args.first;
+        const uint32_t tiles = (uint32_t)p.tiles_i * (uint32_t)p.tiles_j;
+        part = id / tiles;
+        id -= part * tiles;
+    }
+    const int k0 = Op::INT ? 0 : (int)part * p.Kb_split, Kb = Op::INT ? p.Kb : min(p.Kb - k0, p.Kb_split);
     constexpr int BI = TM / 64, BJ = TN / 64, NR = BI + BJ, NS = BI * BJ;
     constexpr int PIECES = SB / 16, RQ = 64 / PIECES;              // pieces of a row in a stage, rows of a request
     constexpr int QA = TM / RQ / 4, QB = TN / RQ / 4, NQ = QA + QB;         // 1 KB requests of a wave per stage
     constexpr int STAGE = (TM + TN) * SB, STEPS = SB / 32;
-    constexpr int TURN = 2 * TM * ((TN / 2 * (int)sizeof(typename E::mem) < 256 ? TN / 2 * (int)sizeof(typename E::mem) : 256) + 16);
-    constexpr int LDS_BYTES = NB * STAGE > TURN ? NB * STAGE : TURN;
+    constexpr int LDS_BYTES = tile_larger(NB * STAGE, tile_larger(turn_bytes<E, TM, TN>, Op::INT ? 0 : turn_bytes<F32, TM, TN>));
     __shared__ __align__(1024) char lds[LDS_BYTES];
     constexpr int SIDE_N = Op::INT ? TM + 2 * TN : TM;
     __shared__ __align__(16) float side[SIDE_N];            // s_i, s_j, bias of the tile, or the bits of exp_i
     typedef __attribute__((address_space(3))) void *lds_ptr_t;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ti, tj;
-    tile_of(blockIdx.x, (uint32_t)p.tiles_i, (uint32_t)p.tiles_j, ti, tj);
+    tile_of(id, (uint32_t)p.tiles_i, (uint32_t)p.tiles_j, ti, tj);
     const int i0 = (int)ti * TM, j0 = (int)tj * TN;
     const int wi = (wave & 1) * (TM / 2), wj = (wave >> 1) * (TN / 2);
 
@@ -188,8 +286,8 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
         };
         // one step: the matrix instructions of `cur`, between them the reads of `next` and a share of a stage's requests.  (All of a
         // stage's requests in one step kept the four waves waiting for the memory pipe, which takes 64 bytes a clock.)
-        auto step = [&](const i32x4_t(&cur)[NR], i32x4_t(&next)[NR], int rbuf, int rstep, auto request, auto part, int dbuf) {
-            constexpr int Q0 = part.value * NQ / STEPS, Q1 = request.value ? (part.value + 1) * NQ / STEPS : Q0;
+        auto step = [&](const i32x4_t(&cur)[NR], i32x4_t(&next)[NR], int rbuf, int rstep, auto request, auto share, int dbuf) {
+            constexpr int Q0 = share.value * NQ / STEPS, Q1 = request.value ? (share.value + 1) * NQ / STEPS : Q0;
 #pragma unroll
             for (int k = 0; k < NS; ++k) {
                 // (the reads are back before the next step begins)
@@ -311,73 +409,17 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const TilePa
         }
     }
 
-    // Register v of lane l holds column 8 (v / 4) + 4 (l / 32) + v % 4 of row l % 32 of a 32 x 32 block.  A wave turns its outputs through
-    // LDS, up to 256 bytes of every row at a time, so that a store is 16 bytes of a lane and a row's pieces lie together.
-    constexpr int WI = TM / 2, WJ = TN / 2, SIZE = (int)sizeof(typename E::mem);
-    constexpr int CB = WJ * SIZE < 256 ? WJ : 256 / SIZE;          // columns at a time
-    constexpr int ROW = CB * SIZE + 16;                            // (rows start in different banks)
-    constexpr int PL = piece_len<E>, LANES = CB / PL;              // lanes that store a row
-    static_assert(4 * WI * ROW <= LDS_BYTES, "the turned outputs of four waves");
 #pragma unroll
     for (int u = 0; u < SIDE; ++u)
         if (u * TILE_THREADS + (int)threadIdx.x < SIDE_N) side[u * TILE_THREADS + threadIdx.x] = side_v[u];
     __syncthreads();                        // (and every wave has read its last fragments)
-    char *const turn = lds + wave * (WI * ROW);
-    typename E::mem *const c = static_cast<typename E::mem *>(p.c) + (size_t)blockIdx.y * (size_t)p.I * (size_t)p.J;
-    const float floor = int8_floor(p.act);
-    const bool whole = i0 + TM <= p.I && j0 + TN <= p.J;
-#pragma unroll
-    for (int cb = 0; cb < WJ / CB; ++cb) {
-#pragma unroll
-        for (int bi = 0; bi < BI; ++bi) {
-            const float s_i = side[wi + 32 * bi + (lane & 31)];
-#pragma unroll
-            for (int bj = cb * (CB / 32); bj < (cb + 1) * (CB / 32); ++bj) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int col = 32 * bj + 8 * g + 4 * (lane >> 5);
-                    float y[4];
-                    if constexpr (Op::INT) {
-                        const tile_f32x4_t sv = *reinterpret_cast<const tile_f32x4_t *>(&side[TM + wj + col]);
-                        const tile_f32x4_t bv = *reinterpret_cast<const tile_f32x4_t *>(&side[TM + TN + wj + col]);
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) y[v] = int8_finish<TANH>(acc[bi][bj][4 * g + v], s_i, sv[v], bv[v], floor, p.act);
-                    } else {
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) y[v] = __builtin_amdgcn_ldexpf(acc[bi][bj][4 * g + v], __float_as_int(s_i));
-                    }
-                    typedef typename E::mem quad_t __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<quad_t *>(turn + (32 * bi + (lane & 31)) * ROW + (col - cb * CB) * SIZE) =
-                        quad_t{E::store(y[0]), E::store(y[1]), E::store(y[2]), E::store(y[3])};
-                }
-            }
+    if constexpr (!Op::INT && !std::is_same_v<E, F32>) {
+        if (p.parts) {
+            tile_output<Op, F32, TM, TN, false, LDS_BYTES>(p, acc, lds, side, i0, j0, part);
+            return;
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");       // (a wave's own outputs: no barrier)
-        const int r0 = lane / LANES, col = (lane % LANES) * PL, j = j0 + wj + cb * CB + col;
-        const char *from = turn + r0 * ROW + col * SIZE;
-        typename E::mem *to = c + (size_t)(i0 + wi + r0) * (size_t)p.J + (size_t)j;
-        const size_t next = (size_t)(64 / LANES) * (size_t)p.J;
-        typedef i32x4_t piece_t __attribute__((aligned(2)));       // (a row starts at any element)
-        if (whole && p.stream) {        // (outputs beyond the caches: 6400 x 512 -> 2048 fp32 20.0 -> 18.2 us)
-#pragma unroll 8
-            for (int u = 0; u < WI * LANES / 64; ++u, from += 64 / LANES * ROW, to += next)
-                __builtin_nontemporal_store(*reinterpret_cast<const i32x4_t *>(from), reinterpret_cast<piece_t *>(to));
-        } else if (whole) {
-#pragma unroll 8
-            for (int u = 0; u < WI * LANES / 64; ++u, from += 64 / LANES * ROW, to += next) *reinterpret_cast<piece_t *>(to) = *reinterpret_cast<const i32x4_t *>(from);
-        } else {
-#pragma unroll 1
-            for (int i = i0 + wi + r0; i < min(p.I, i0 + wi + WI); i += 64 / LANES, from += 64 / LANES * ROW, to += next) {
-                if (j + PL <= p.J) {
-                    *reinterpret_cast<piece_t *>(to) = *reinterpret_cast<const i32x4_t *>(from);
-                } else {
-#pragma unroll 1
-                    for (int x = 0; j + x < p.J; ++x) to[x] = reinterpret_cast<const typename E::mem *>(from)[x];
-                }
-            }
-        }
-        if (cb + 1 < WJ / CB) asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
     }
+    tile_output<Op, E, TM, TN, TANH, LDS_BYTES>(p, acc, lds, side, i0, j0, part);
 }
 
 }  // namespace adapt

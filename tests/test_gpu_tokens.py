@@ -331,6 +331,28 @@ def test_int8_linear_backward_long_sums(B, M, K, N):
         within(db, wb, mb, M, name)
 
 
+# sizes at which the gradients' sums are split (both; only dx's; only dw's, up to 64 parts) and their products share a launch or do not
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", [(1287, 3, 1675), (64, 130, 2300), (2300, 130, 64), (70000, 20, 24), (24, 20, 70000), (1067, 861, 1722),
+                                   (55492, 4, 54), (2900, 384, 700)])
+def test_int8_linear_backward_has_the_same_bits_whatever_is_asked_for(B, name, M, K, N):
+    import torch
+    rng = np.random.default_rng(M + N)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    dy, dyd = randn(rng, (M, N), name)
+    operands = (dyd, dev(a), dev(s_a), dev(w), dev(s_w))
+    dx, dw, db = B.adapt_int8_linear_backward(*operands)
+    (wx, mx), (ww, mw), (wb, mb) = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+    within(dx, wx, mx, N, name, KEPT[name], far_below(dy * s_w, w))
+    within(dw, ww, mw, M, name, KEPT[name], far_below((dy * s_a[:, None]).T, a))
+    within(db, wb, mb, M, name)
+    for want in (("dx",), ("dw",), ("dx", "db"), ("dw", "db"), ("dx", "dw")):
+        for got, full, key in zip(B.adapt_int8_linear_backward(*operands, want=want), (dx, dw, db), ("dx", "dw", "db")):
+            assert (got is None) == (key not in want)
+            if got is not None:
+                same_bits(got, full.cpu())
+
+
 def test_int8_linear_backward_infinities_and_nan_stay_in_their_rows(B):
     import torch
     rng = np.random.default_rng(9)

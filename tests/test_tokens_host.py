@@ -143,6 +143,22 @@ def test_workspaces_grow_with_the_call(lib):
         assert sizes == sorted(sizes) and sizes[-1] > sizes[0]
 
 
+def test_int8_linear_backward_workspace_for_both_is_enough_for_one(lib):
+    n = ctypes.c_size_t()
+
+    def need(M, K, N, t, dx, dw):
+        assert lib.adapt_int8_linear_backward_workspace(M, K, N, t, dx, dw, ctypes.byref(n)) == 0
+        return n.value
+    sizes = (0, 1, 63, 64, 700, 6400, 100000, 1 << 21)
+    for M in sizes:
+        for K in (0, 1, 20, 512, 4096):
+            for N in sizes:
+                if M * N < 1 << 34 and M * K < 1 << 34 and N * K < 1 << 34:
+                    for t in (0, 1, 2):
+                        both, dx, dw, db = (need(M, K, N, t, x, w) for x, w in ((1, 1), (1, 0), (0, 1), (0, 0)))
+                        assert both == dx + dw - db >= max(dx, dw) and db > 0 or not N
+
+
 # ---- the oracle itself
 
 def test_philox_known_answers():
