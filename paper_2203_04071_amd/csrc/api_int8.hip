@@ -56,7 +56,8 @@ void launch_tiles(TileKind kind, const Params &p, const Tiles &t, hipStream_t s)
         case TILE_128x128: launch_tile<E, 128, 128, 128, 4, true>(p, t, s); break;
         case TILE_128x128_TWO: launch_tile<E, 128, 128, 64, 3, true>(p, t, s); break;
         case TILE_128x64: launch_tile<E, 128, 64, 128, 4, true>(p, t, s); break;
-        default: launch_tile<E, 64, 64, 128, 4, true>(p, t, s); break;
+        case TILE_64x64: launch_tile<E, 64, 64, 128, 4, true>(p, t, s); break;
+        default: launch_tile<E, 64, 64, 64, 3, true>(p, t, s); break;
     }
 }
 

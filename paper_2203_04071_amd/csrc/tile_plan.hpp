@@ -4,7 +4,7 @@
 
 namespace adapt_api {
 
-enum TileKind { TILE_256x256, TILE_256x128, TILE_128x128, TILE_128x128_TWO, TILE_128x64, TILE_64x64, TILE_KINDS };       // _TWO: on a compute unit at a time
+enum TileKind { TILE_256x256, TILE_256x128, TILE_128x128, TILE_128x128_TWO, TILE_128x64, TILE_64x64, TILE_64x64_SIX, TILE_KINDS };       // _TWO, _SIX: on a compute unit at a time
 
 struct TilePlan {
     TileKind kind;
@@ -15,22 +15,27 @@ struct TilePlan {
 };
 
 // Times in microseconds: a stage (128 bytes of every row) of a workgroup that has a compute unit to itself, everything else of a tile
-// (first requests, outputs), workgroups that a compute unit's LDS holds.  Measured on 2048 x 512 outputs over 300 stages (stages) and
-// 6400 x 2048 fp32 outputs over 4 (the rest).  Whole products:
-//                                          256x256  256x128  128x128  _TWO  128x64  64x64
-//     8192 x 8192, 64 stages int8 -> bf16     469      487      596    707     804    881 us
-//     4096 x 4096, 128 stages bf16            210      221      248    321     361     -
-//     2048 x 512, 300 stages bf16             309      161      104    160      83     -
-//     6400 x 512, 96 stages bf16              107       62       43     55      62     -
-//     1111 x 999, 32 stages int8               50       28       18     20      14    13
-//     6400 x 2048, 4 stages int8 -> fp32       21       22       24     18      26    19
+// (first requests, outputs), workgroups that a compute unit's LDS holds.  Small tiles hide the outputs of one behind the sums of others, large ones
+// read the operands less often.  Measured on 2048 x 512 outputs over 300 stages (stages) and 6400 x 2048 fp32 outputs over 4 (the rest); those with
+// several on a compute unit fitted to 177 drawn int8 products, for which the plan is 1.0 % slower than the best kind (6 % without _SIX).
+//                                          256x256  256x128  128x128  _TWO  128x64  64x64  _SIX
+//     8192 x 8192, 64 stages int8 -> bf16     469      487      596    707     804    881     -  us
+//     4096 x 4096, 32 stages int8 -> bf16      63       63       72     80      98    106   152
+//     2048 x 512, 300 stages bf16             309      161      104    160      83     -      -
+//     6400 x 512, 96 stages bf16              107       62       43     55      62     -      -
+//     1111 x 999, 32 stages int8               50       28       18     20      14    13     21
+//     6400 x 2048, 4 stages int8 -> fp32       20       22       24     19      29    24     21
+//     1300 x 9615, 2 stages int8 -> fp32       29       24       23     23      27    21     16
+//     20000 x 512, 1 stage int8 -> fp16        13       14       13     11      15    13    9.6
 struct TileCost {
     int tm, tn;
     double stage, rest;
     int per_cu;
+    double alone;       // times of a stage that it takes however few workgroups share a compute unit
 };
-constexpr TileCost TILE_COST[TILE_KINDS] = {{256, 256, 1.03, 14.0, 1}, {256, 128, 0.54, 7.5, 1}, {128, 128, 0.35, 4.2, 1},
-                                            {128, 128, 0.54, 4.0, 2},  {128, 64, 0.27, 2.3, 1},  {64, 64, 0.17, 1.1, 2}};
+constexpr TileCost TILE_COST[TILE_KINDS] = {{256, 256, 1.03, 14.0, 1, 1.0}, {256, 128, 0.54, 7.5, 1, 1.0}, {128, 128, 0.35, 4.2, 1, 1.0},
+                                            {128, 128, 0.59, 2.6, 2, 1.0},  {128, 64, 0.27, 2.3, 1, 1.0},  {64, 64, 0.20, 1.9, 2, 1.0},
+                                            {64, 64, 0.22, 0.5, 6, 3.0}};
 
 // A way to share a product out: tiles of a kind, rows in `split` parts of `part` stages, `groups` workgroups.
 struct TileWay {
@@ -62,9 +67,10 @@ inline int tile_ways(const TileCost &c, long long I, long long J, long long stag
 inline TilePlan tile_plan_of(int kind, const TileWay &w, long long Kb) {
     return TilePlan{(TileKind)kind, TILE_COST[kind].tm, TILE_COST[kind].tn, w.ti, w.tj, w.split, w.split > 1 ? w.part * 128 : Kb};
 }
-// two workgroups on a compute unit share what one has
+// workgroups on a compute unit share what one has; _SIX's have too little on its way to take it all
 inline double tile_shared(const TileCost &c, long long groups, int cus) {
-    return c.per_cu == 1 || groups <= cus ? 1.0 : (groups >= 2ll * cus ? 2.0 : (double)groups / cus);
+    const double n = groups >= (long long)c.per_cu * cus ? c.per_cu : (double)groups / cus;
+    return n > c.alone ? n : c.alone;
 }
 
 // Kb: bytes of a row; split as above

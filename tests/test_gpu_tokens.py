@@ -180,6 +180,17 @@ def test_int8_linear(B, name, M, K, N):
     same_bits(B.adapt_int8_linear(ad, sad, wd, swd, bias=dev(bias), act=1, dtype=_t(name)), rounded(ot.int8_linear(a, s_a, w, s_w, bias, 1), name))
 
 
+# rows of one to four stages, whole and not, and many outputs: the small tiles of which a compute unit holds several
+@pytest.mark.parametrize("M,K,N", [(300, 80, 1300), (1000, 16, 1000), (700, 112, 900), (513, 208, 1025), (6400, 64, 512), (130, 48, 9000), (2000, 128, 777)])
+def test_int8_linear_short_rows(B, M, K, N):
+    rng = np.random.default_rng(M + K)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    bias = rng.standard_normal(N).astype(np.float32)
+    for name in TYPES:
+        got = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), bias=dev(bias), act=1, dtype=_t(name))
+        same_bits(got, rounded(ot.int8_linear(a, s_a, w, s_w, bias, 1), name))
+
+
 @pytest.mark.parametrize("M,K,N", [(1, 512, 64), (40, 300, 70), (300, 256, 300)])
 def test_int8_linear_tanh_and_scales_as_they_come(B, M, K, N):
     """tanh is the library's own; scales of zero, infinity and NaN go through the formula."""
