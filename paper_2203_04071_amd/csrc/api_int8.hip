@@ -72,11 +72,18 @@ void launch_tokens(const adapt::Int8Params &p, hipStream_t s) {
     else adapt::int8_tokens_kernel<E, MT, 8, false, TANH><<<grid, 512, 0, s>>>(p);
 }
 
-// Rows that no 16-byte piece divides: 64 x 64 outputs in stages of 64 bytes, or 128 x 64 in stages of 128 (half the LDS traffic and two thirds of the
-// requests) where the sums are long or the tiles many: 1111 x 777 -> 999 9.7 us against 11.4, 1111 x 4095 -> 999 30 against 26,
-// 4000 x 1999 -> 2000 64 against 52.
-bool long_ragged(const adapt::TileParams &p) {
-    return p.Kb >= 2048 || ((p.I + 127ll) / 128) * ((p.J + 63ll) / 64) >= device_cus();
+// Rows that no 16-byte piece divides: 64 x 64 outputs in stages of 64 bytes, several on a compute unit.  Fewer requests an output where the tiles are many
+// and the sums not short (128 x 128) or the sums long (128 x 64 in stages of 128 bytes).  64 x 64, 128 x 64, 128 x 128 (us):
+//     1111 x 777 -> 999 fp32       10.4  11.5  14.1        4000 x 1999 -> 2000 fp32    66   50   44
+//     5952 x 167 -> 4096 fp16      36    43    34          4000 x 4001 -> 4000 bf16   227  164  140
+//     7633 x 113 -> 5504 fp32      53    64    60          1111 x 4095 -> 999 bf16     31   26   38
+//     20000 x 100 -> 500 fp16      12.5  15.2  17.9        556 x 2885 -> 576 fp32      14   19   25
+template <class E>
+void launch_ragged(const adapt::TileParams &p, hipStream_t s) {
+    const TilePlan large = one_tile(p.I, p.J, p.Kb, 128, 128), middle = one_tile(p.I, p.J, p.Kb, 128, 64);
+    if (p.Kb >= 512 && 2 * large.tiles_i * large.tiles_j >= 3 * device_cus()) launch_tile<E, 128, 128, 64, 2, false>(p, large, s);
+    else if (p.Kb >= 2048 && middle.tiles_i * middle.tiles_j >= device_cus() / 2) launch_tile<E, 128, 64, 128, 2, false>(p, middle, s);
+    else launch_tile<E, 64, 64, 64, 2, false>(p, one_tile(p.I, p.J, p.Kb, 64, 64), s);
 }
 
 // Few tokens, or few tiles: the kernel without LDS tiles (int8_tokens_kernel) reads 16 (MT + 1) K bytes per workgroup of 16 x 16 MT outputs, at about
@@ -138,8 +145,9 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
     if (dma) {
         const TilePlan t = tile_plan(p.I, p.J, p.Kb, device_cus(), 1);
         launch_tiles<E>(t.kind, p, t, s);
-    } else if (long_ragged(p)) launch_tile<E, 128, 64, 128, 2, false>(p, one_tile(p.I, p.J, p.Kb, 128, 64), s);
-    else launch_tile<E, 64, 64, 64, 2, false>(p, small, s);
+    } else {
+        launch_ragged<E>(p, s);
+    }
 }
 
 int grad_whole(long long R) { return (int)((R + adapt::GRAD_STAGE - 1) / adapt::GRAD_STAGE * adapt::GRAD_STAGE); }

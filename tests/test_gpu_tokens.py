@@ -180,6 +180,17 @@ def test_int8_linear(B, name, M, K, N):
     same_bits(B.adapt_int8_linear(ad, sad, wd, swd, bias=dev(bias), act=1, dtype=_t(name)), rounded(ot.int8_linear(a, s_a, w, s_w, bias, 1), name))
 
 
+# rows that no 16-byte piece divides: many outputs and long enough sums; long sums; neither
+@pytest.mark.parametrize("M,K,N", [(2050, 515, 4100), (1027, 2049, 1100), (1500, 513, 700), (4100, 31, 2050), (600, 2051, 130)])
+def test_int8_linear_ragged_rows(B, M, K, N):
+    rng = np.random.default_rng(M + K)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M), scales(rng, N)
+    bias = rng.standard_normal(N).astype(np.float32)
+    for name in TYPES:
+        got = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), bias=dev(bias), dtype=_t(name))
+        same_bits(got, rounded(ot.int8_linear(a, s_a, w, s_w, bias), name))
+
+
 # rows of one to four stages, whole and not, and many outputs: the small tiles of which a compute unit holds several
 @pytest.mark.parametrize("M,K,N", [(300, 80, 1300), (1000, 16, 1000), (700, 112, 900), (513, 208, 1025), (6400, 64, 512), (130, 48, 9000), (2000, 128, 777)])
 def test_int8_linear_short_rows(B, M, K, N):
