@@ -255,7 +255,8 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const typena
 
     if constexpr (DMA) {
         int dma_s = 0;          // stage that is requested next
-        int kb = Op::INT ? 0 : k0 % p.Kb_b;
+        const int Kb_b = p.Kb_b;        // (a copy: the parameters of a pair would be read again in every stage)
+        int kb = Op::INT ? 0 : k0 % Kb_b;
         const char *da = abase, *db = bbase + kb;
         auto dma_begin = [&]() {        // where the last stage is not whole, lanes whose piece lies behind the end fetch its first piece instead
             if (Op::INT && dma_s == full && piece16 >= rest)
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const typena
             ++dma_s;
             if constexpr (!Op::INT) {
                 kb += SB;
-                if (kb == p.Kb_b) {
+                if (kb == Kb_b) {
                     kb = 0;
                     db = bbase;
                 }
