@@ -556,7 +556,7 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
  * far below the largest of their sum's to 2^-40 of that largest; sums are fp32.
  * M, K and N are at most 2^21 and no matrix has 2^34 elements, else ADAPT_ERR_UNSUPPORTED.
  * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
- * dx_dev / dw_dev are given). */
+ * dx_dev / dw_dev are given; what is reported for both is enough for one).  A gradient has the same bits whatever else is asked for. */
 int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want_dx, int want_dw, size_t *bytes);
 int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev,
                                int M, int K, int N, void *dx_dev, void *dw_dev, void *db_dev, void *workspace_dev, size_t workspace_bytes,

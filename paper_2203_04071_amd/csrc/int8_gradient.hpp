@@ -8,8 +8,8 @@
 // two, t = t0 + t1, t1 the rest that t0 leaves (22 bits: fp16 and fp32 gradients; 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at
 // every addition).  Elements below 2^-18 (22 bits) or 2^-29 (11 bits) of their row's largest keep fewer bits; what they lose is below 2^-40 of that largest.  So a
 // gradient is an fp16 product with exact partial products and fp32 sums over rows [t1 | t0] that meet the same codes twice, the small pieces first.
-// (Three bf16 pieces of 24 bits, without the rows' powers of two, took 148 us where this takes 124 for 6400 x 512 -> 2048 fp32; two of them 470 us
-// against 287 for 4096^3 bf16.)
+// (Three bf16 pieces of 24 bits, without the rows' powers of two, took 148 us where this takes 114 for 6400 x 512 -> 2048 fp32; two of them 470 us
+// against 281 for 4096^3 bf16.)
 //
 // Both matrices are written to the workspace with the summed index last, rows in whole stages of 128 bytes.
 #pragma once
