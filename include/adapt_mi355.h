@@ -552,8 +552,8 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
  *     db[n]    = sum_m dy[m][n]
  * dy_dev [M][N], dx_dev [M][K], dw_dev [N][K], db_dev [N] of element type `type`; codes and scales as in adapt_int8_linear.  Any of dx_dev,
  * dw_dev, db_dev may be NULL (not computed; a_dev and s_a_dev are read for dw alone, w_dev and s_w_dev for dx alone).  They are
- * fully overwritten.  dy * s is formed in fp32 and kept to 22 bits (ADAPT_F32, ADAPT_F16) or 11 bits (ADAPT_BF16, whose results keep 8), elements
- * far below the largest of their sum's to 2^-40 of that largest; sums are fp32.
+ * fully overwritten.  dy * s is formed in fp32 and kept to 22 bits, elements far below the largest of their sum's to 2^-40 of that largest; sums are
+ * fp32.
  * M, K and N are at most 2^21 and no matrix has 2^34 elements, else ADAPT_ERR_UNSUPPORTED.
  * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
  * dx_dev / dw_dev are given; what is reported for both is enough for one).  A gradient has the same bits whatever else is asked for. */

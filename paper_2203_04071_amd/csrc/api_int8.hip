@@ -15,7 +15,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int INT8_MAX_K = 131071;              // (-128)^2 K < 2^31
 constexpr long long MAX_TILES = 1ll << 24;      // a launch is limited to 2^32 threads
 constexpr int TOKENS_GROUPS = 1 << 23;         // the same for workgroups of 512
-constexpr int GRAD_MAX = 2097152;               // 256 rows of its pieces (6 bytes an element) are addressed with 32 bits
+constexpr int GRAD_MAX = 2097152;               // 256 rows of its pieces (4 bytes an element) are addressed with 32 bits
 
 int int8_args(const char *who, int M, int K, int N, int type) {
     if (M < 0 || K < 0 || N < 0) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: negative size", who);
@@ -161,10 +161,10 @@ struct GradPlan {
     size_t b, exps, part, bytes;    // offsets (a at 0)
 };
 // (the tile comes from grad_plans)
-GradPlan grad_plan(long long I, long long J, long long R, int P, const TilePlan &tile) {
+GradPlan grad_plan(long long I, long long J, long long R, const TilePlan &tile) {
     GradPlan g{};
     g.Rp = grad_whole(R);
-    g.row = 2ll * P * g.Rp;
+    g.row = 2ll * adapt::GRAD_PIECES * g.Rp;
     g.row_b = 2ll * g.Rp;
     g.tile = tile;
     g.b = round256((size_t)I * (size_t)g.row);
@@ -173,7 +173,6 @@ GradPlan grad_plan(long long I, long long J, long long R, int P, const TilePlan 
     g.bytes = g.part + (g.tile.split > 1 ? round256((size_t)g.tile.split * (size_t)I * (size_t)J * 4) : 0);
     return g;
 }
-int grad_pieces(int type) { return type == ADAPT_BF16 ? 1 : 2; }
 
 // partial results of the columns, sums and largest elements: rows that a block takes, blocks, bytes
 int column_rows(int M) {
@@ -190,9 +189,9 @@ struct GradPlans {
     int first;                  // 1: dw's workgroups come first
     size_t bytes;
 };
-GradPlans grad_plans(int M, int K, int N, int type, bool want_dx, bool want_dw) {
-    const int P = grad_pieces(type), cus = device_cus();
-    const long long I[2] = {M, N}, J[2] = {K, K}, Kb[2] = {2ll * P * grad_whole(N), 2ll * P * grad_whole(M)};
+GradPlans grad_plans(int M, int K, int N, bool want_dx, bool want_dw) {
+    const int cus = device_cus();
+    const long long I[2] = {M, N}, J[2] = {K, K}, Kb[2] = {2ll * adapt::GRAD_PIECES * grad_whole(N), 2ll * adapt::GRAD_PIECES * grad_whole(M)};
     // (a gradient has the same bits whatever else is asked for: the number of parts is the pair's, the tile that which is best for it alone)
     TilePairPlan t = tile_pair_plan(I, J, Kb, cus);
     if (!want_dx || !want_dw) {
@@ -200,8 +199,8 @@ GradPlans grad_plans(int M, int K, int N, int type, bool want_dx, bool want_dw) 
         for (int x = 0; x < 2; ++x) t.plan[x] = tile_plan(I[x], J[x], Kb[x], cus, t.plan[x].split);
     }
     GradPlans g{};
-    if (want_dx) g.x = grad_plan(M, K, N, P, t.plan[0]);
-    if (want_dw) g.w = grad_plan(N, K, M, P, t.plan[1]);
+    if (want_dx) g.x = grad_plan(M, K, N, t.plan[0]);
+    if (want_dw) g.w = grad_plan(N, K, M, t.plan[1]);
     g.joint = t.joint;
     g.first = t.first;
     g.bytes = g.x.bytes + g.w.bytes + column_bytes(M, N);
@@ -235,18 +234,18 @@ void grad_join(const GradPlan &g, const char *ws, int I, int J, void *c, hipStre
 
 // a wave per row up to 1024 elements, a workgroup up to 8192 (quantize_tokens has the like); a workgroup takes several rows, whose scales of the
 // columns it reads once
-template <class E, int P>
+template <class E>
 void prepare(const adapt::GradPrep &p, unsigned groups, hipStream_t s) {
     constexpr int T = adapt::GRAD_THREADS;
-    if (p.Np <= 512) adapt::grad_prepare_kernel<E, P, 64, 1><<<groups, T, 0, s>>>(p);
-    else if (p.Np <= 1024) adapt::grad_prepare_kernel<E, P, 64, 2><<<groups, T, 0, s>>>(p);
-    else if (p.Np <= 2048) adapt::grad_prepare_kernel<E, P, T, 1><<<groups, T, 0, s>>>(p);
-    else if (p.Np <= 4096) adapt::grad_prepare_kernel<E, P, T, 2><<<groups, T, 0, s>>>(p);
-    else if (p.Np <= 8192) adapt::grad_prepare_kernel<E, P, T, 4><<<groups, T, 0, s>>>(p);
-    else adapt::grad_prepare_kernel<E, P, 0, 0><<<groups, T, 0, s>>>(p);
+    if (p.Np <= 512) adapt::grad_prepare_kernel<E, 64, 1><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 1024) adapt::grad_prepare_kernel<E, 64, 2><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 2048) adapt::grad_prepare_kernel<E, T, 1><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 4096) adapt::grad_prepare_kernel<E, T, 2><<<groups, T, 0, s>>>(p);
+    else if (p.Np <= 8192) adapt::grad_prepare_kernel<E, T, 4><<<groups, T, 0, s>>>(p);
+    else adapt::grad_prepare_kernel<E, 0, 0><<<groups, T, 0, s>>>(p);
 }
 
-template <class E, int P>
+template <class E>
 void gradients(const adapt::Int8Params &q, const GradPlans &plans, const void *dy, void *dx, void *dw, void *db_dev, char *ws, hipStream_t s) {
     typedef typename E::mem mem;
     mem *const db = static_cast<mem *>(db_dev);
@@ -287,14 +286,14 @@ void gradients(const adapt::Int8Params &q, const GradPlans &plans, const void *d
         a_groups = p.a_blocks * blocks(q.K);
     }
     const uint32_t groups = p.row_groups + p.w_groups + p.column_groups + a_groups;
-    if (groups) prepare<E, P>(p, groups, s);
+    if (groups) prepare<E>(p, groups, s);
     adapt::TileParams px{}, pw{};
     if (dx) px = grad_params(gx, wx, q.M, q.K, dx, sizeof(mem));
     if (dw) pw = grad_params(gw, ww, q.N, q.K, dw, sizeof(mem));
     const unsigned nx = grad_groups(gx), nw = grad_groups(gw);
     if (dx && !plans.joint) launch_tiles<E>(gx.tile.kind, adapt::TilePair{{px, px}, nx}, nx, s);
     if (dw && gw.Rp) {
-        adapt::grad_turned_rows_kernel<E, P><<<dim3((unsigned)gw.Rp / 64, blocks(q.N)), 256, 0, s>>>(
+        adapt::grad_turned_rows_kernel<E><<<dim3((unsigned)gw.Rp / 64, blocks(q.N)), 256, 0, s>>>(
             static_cast<const mem *>(dy), q.s_a, p.sum, p.big, db, reinterpret_cast<int *>(ww + gw.exps), reinterpret_cast<_Float16 *>(ww), q.M, q.N, gw.Rp,
             column_blocks(q.M));
     } else {
@@ -336,7 +335,7 @@ int adapt_int8_linear_backward_workspace(int M, int K, int N, int type, int want
     *bytes = 0;
     if (int rc = int8_args(who, M, K, N, type)) return rc;
     if (int rc = grad_limits(who, M, K, N)) return rc;
-    *bytes = grad_plans(M, K, N, type, want_dx && M && K, want_dw && N && K).bytes;
+    *bytes = grad_plans(M, K, N, want_dx && M && K, want_dw && N && K).bytes;
     return ADAPT_OK;
 }
 
@@ -357,7 +356,7 @@ int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev
         if (g && (g == dy_dev || g == (const void *)a_dev || g == (const void *)w_dev))
             return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
     if (int rc = grad_limits(who, M, K, N)) return rc;
-    const GradPlans plans = grad_plans(M, K, N, type, want_dx, want_dw);
+    const GradPlans plans = grad_plans(M, K, N, want_dx, want_dw);
     const size_t need = plans.bytes;
     if (need && (!workspace_dev || workspace_bytes < need || off_by(workspace_dev, 256)))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, need);
@@ -365,9 +364,7 @@ int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev
     char *const ws = static_cast<char *>(workspace_dev);
     void *const dx = want_dx ? dx_dev : nullptr, *const dw = want_dw ? dw_dev : nullptr, *const db = want_db ? db_dev : nullptr;
     hipStream_t s = (hipStream_t)stream;
-    if (type == ADAPT_F32) gradients<adapt::F32, 2>(p, plans, dy_dev, dx, dw, db, ws, s);
-    else if (type == ADAPT_F16) gradients<adapt::F16, 2>(p, plans, dy_dev, dx, dw, db, ws, s);
-    else gradients<adapt::BF16, 1>(p, plans, dy_dev, dx, dw, db, ws, s);
+    ADAPT_FOR_TYPE(type, E, gradients<E>(p, plans, dy_dev, dx, dw, db, ws, s));
     HIP_TRY(hipGetLastError());
     return ADAPT_OK;
 }

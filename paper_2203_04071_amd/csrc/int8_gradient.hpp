@@ -3,13 +3,12 @@
 //     dx[m][k] = sum_n (dy[m][n] s_w[n]) w[n][k],      dw[n][k] = sum_m (dy[m][n] s_a[m]) a[m][k]
 //
 // Both are c[i][j] = sum_r t[i][r] q[j][r] with codes q, which are fp16 numbers.  t = dy s becomes fp16 numbers as well: every row i is brought to
-// a largest element in [2^14, 2^15) by a power of two, which goes back in on the sums, and is then one fp16 number (11 bits: bf16 gradients, whose
-// results keep 8; a term is off by 2^-11 of itself at most, independently of the others, where the result is rounded by 2^-8) or the sum of
-// two, t = t0 + t1, t1 the rest that t0 leaves (22 bits: fp16 and fp32 gradients; 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at
-// every addition).  Elements below 2^-18 (22 bits) or 2^-29 (11 bits) of their row's largest keep fewer bits; what they lose is below 2^-40 of that largest.  So a
-// gradient is an fp16 product with exact partial products and fp32 sums over rows [t1 | t0] that meet the same codes twice, the small pieces first.
-// (Three bf16 pieces of 24 bits, without the rows' powers of two, took 148 us where this takes 114 for 6400 x 512 -> 2048 fp32; two of them 470 us
-// against 281 for 4096^3 bf16.)
+// a largest element in [2^14, 2^15) by a power of two, which goes back in on the sums, and is then the sum of two fp16 numbers, t = t0 + t1, t1 the
+// rest that t0 leaves: 22 bits, 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at every addition.  Elements below 2^-18 of their row's
+// largest keep fewer bits; what they lose is below 2^-40 of that largest.  So a gradient is an fp16 product with exact partial products and fp32 sums over
+// rows [t1 | t0] that meet the same codes twice, the small pieces first.  (One piece of 11 bits is half the work, 288 us against 508 for 4096^3 bf16, but
+// leaves a bf16 gradient none of its 8 bits where the terms of a sum cancel to 2^-12 of themselves.  Three bf16 pieces of 24 bits, without the rows'
+// powers of two, took 148 us where this takes 114 for 6400 x 512 -> 2048 fp32.)
 //
 // Both matrices are written to the workspace with the summed index last, rows in whole stages of 128 bytes.
 #pragma once
@@ -26,28 +25,19 @@ __device__ __forceinline__ int grad_exponent(float m) {
     return (m < __builtin_inff() ? __builtin_amdgcn_frexp_expf(m) : 128) - 15;
 }
 
-// piece z = 0 (the smaller) .. P - 1 of t 2^-e
-template <int P>
-__device__ __forceinline__ void split_pieces(float t, int e, _Float16 (&out)[P]) {
-    t = __builtin_amdgcn_ldexpf(t, -e);
-    out[P - 1] = (_Float16)t;
-    if constexpr (P == 2) {
-        const float hi = (float)out[1];
-        out[0] = fabsf(hi) < __builtin_inff() ? (_Float16)(t - hi) : (_Float16)0.0f;        // (t - hi is exact; infinities and NaN: the first piece alone)
-    }
-}
-template <int P>
-__device__ __forceinline__ void store_pieces(const float (&t)[8], int e, _Float16 *out, size_t next) {      // next: elements to the piece behind
-    f16x8_t v[P];
+// pieces 0 (the smaller) and 1 of eight t 2^-e; next: elements from a piece to the one behind
+constexpr int GRAD_PIECES = 2;
+__device__ __forceinline__ void store_pieces(const float (&t)[8], int e, _Float16 *out, size_t next) {
+    f16x8_t v[GRAD_PIECES];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        _Float16 q[P];
-        split_pieces<P>(t[j], e, q);
-#pragma unroll
-        for (int z = 0; z < P; ++z) v[z][j] = q[z];
+        const float x = __builtin_amdgcn_ldexpf(t[j], -e);
+        v[1][j] = (_Float16)x;
+        const float hi = (float)v[1][j];
+        v[0][j] = fabsf(hi) < __builtin_inff() ? (_Float16)(x - hi) : (_Float16)0.0f;       // (x - hi is exact; infinities and NaN: the larger piece alone)
     }
-#pragma unroll
-    for (int z = 0; z < P; ++z) *reinterpret_cast<f16x8_t *>(out + z * next) = v[z];
+    *reinterpret_cast<f16x8_t *>(out) = v[0];
+    *reinterpret_cast<f16x8_t *>(out + next) = v[1];
 }
 
 // eight elements n .. n + 7 of a row of N, zeros beyond its end
@@ -63,7 +53,7 @@ __device__ __forceinline__ void load_eight(const typename E::mem *__restrict__ r
 
 // out[m][z][n] = piece z of dy[m][n] * s[n], exps[m]; zeros for N <= n < Np.  GROUP lanes share a row, NP times eight elements each, which stay in
 // registers between the maximum and the pieces; a lane's columns are the same in every row, their scales are read once.
-template <typename E, int P, int GROUP, int NP>
+template <typename E, int GROUP, int NP>
 __device__ __forceinline__ void grad_rows(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out, int *__restrict__ exps,
                                           int M, int N, int Np, uint32_t block, uint32_t blocks, float *part) {
     constexpr int WAVES = GROUP / 64;
@@ -95,13 +85,13 @@ __device__ __forceinline__ void grad_rows(const typename E::mem *__restrict__ dy
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
             const int n = (u * GROUP + lane) * 8;
-            if (n < Np) store_pieces<P>(t[u], e, out + (size_t)m * P * (size_t)Np + n, (size_t)Np);
+            if (n < Np) store_pieces(t[u], e, out + (size_t)m * GRAD_PIECES * (size_t)Np + n, (size_t)Np);
         }
     }
 }
 
 // The same for rows too long for registers: read twice.
-template <typename E, int P>
+template <typename E>
 __device__ __forceinline__ void grad_long_rows(const typename E::mem *__restrict__ dy, const float *__restrict__ s, _Float16 *__restrict__ out, int *__restrict__ exps,
                                                int M, int N, int Np, uint32_t block, uint32_t blocks, float *part) {
     for (int m = (int)block; m < M; m += (int)blocks) {
@@ -130,7 +120,7 @@ __device__ __forceinline__ void grad_long_rows(const typename E::mem *__restrict
         for (int n = threadIdx.x * 8; n < Np; n += GRAD_THREADS * 8) {
             float t[8];
             eight(n, t);
-            store_pieces<P>(t, e, out + (size_t)m * P * (size_t)Np + n, (size_t)Np);
+            store_pieces(t, e, out + (size_t)m * GRAD_PIECES * (size_t)Np + n, (size_t)Np);
         }
     }
 }
@@ -239,7 +229,7 @@ __device__ __forceinline__ void grad_transposed(const float (*tile)[GRAD_LD], in
 
 // out[n][z][m] = piece z of dy[m][n] * s[m] 2^-exps[n], the exponents from the row blocks' maxima; the first workgroup of 64 columns also writes
 // exps and, if sum != nullptr, db
-template <typename E, int P>
+template <typename E>
 __global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const typename E::mem *__restrict__ dy, const float *__restrict__ s, const float *__restrict__ sum,
                                                                         const float *__restrict__ big, typename E::mem *__restrict__ db, int *__restrict__ exps,
                                                                         _Float16 *__restrict__ out, int M, int N, int Mp, int blocks) {
@@ -270,7 +260,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_turned_rows_kernel(const ty
     }
     __syncthreads();
     grad_transposed(tile, N, r0, c0, [&](int col, int row, const float(&e)[8]) {
-        store_pieces<P>(e, exponents[col - c0], out + (size_t)col * P * (size_t)Mp + row, (size_t)Mp);
+        store_pieces(e, exponents[col - c0], out + (size_t)col * GRAD_PIECES * (size_t)Mp + row, (size_t)Mp);
     });
 }
 
@@ -314,15 +304,15 @@ struct GradPrep {
     uint32_t row_groups, w_groups, column_groups, w_blocks, column_blocks, a_blocks;    // ranges, the first dimension of three of them
 };
 // GROUP 0: rows too long for registers
-template <typename E, int P, int GROUP, int NP>
+template <typename E, int GROUP, int NP>
 __global__ __launch_bounds__(GRAD_THREADS) void grad_prepare_kernel(const GradPrep p) {
     __shared__ float lds[64 * GRAD_LD];
     static_assert(2 * GRAD_THREADS / (64 / piece_len<E>) * 64 <= 64 * GRAD_LD, "column statistics");
     const typename E::mem *const dy = static_cast<const typename E::mem *>(p.dy);
     uint32_t g = blockIdx.x;
     if (g < p.row_groups) {
-        if constexpr (GROUP == 0) grad_long_rows<E, P>(dy, p.s_w, p.dy_rows, p.row_exps, p.M, p.N, p.Np, g, p.row_groups, lds);
-        else grad_rows<E, P, GROUP, NP>(dy, p.s_w, p.dy_rows, p.row_exps, p.M, p.N, p.Np, g, p.row_groups, lds);
+        if constexpr (GROUP == 0) grad_long_rows<E>(dy, p.s_w, p.dy_rows, p.row_exps, p.M, p.N, p.Np, g, p.row_groups, lds);
+        else grad_rows<E, GROUP, NP>(dy, p.s_w, p.dy_rows, p.row_exps, p.M, p.N, p.Np, g, p.row_groups, lds);
         return;
     }
     g -= p.row_groups;

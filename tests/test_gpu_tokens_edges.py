@@ -1,0 +1,53 @@
+"""Token-wise operators where their definition is easiest to miss: sums whose terms cancel."""
+import numpy as np
+import pytest
+
+from oracle import tokens as ot
+from test_gpu_tokens import TYPES, U, B, _t, codes, dev, f64, far_below, rounded, scales  # noqa: F401  (B: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------- gradients of the product
+
+def within_22_bits(got, want, mass, terms, name, lost):
+    """A gradient of any type: dy * s to 22 bits (2^-22 of a term), sums of fp32, one rounding to the type at the end.  mass: sum of |terms|."""
+    import torch
+    fi = torch.finfo(_t(name))
+    bound = ((terms + 2) * U + 2.0 ** -22) * mass + lost + 2.0 ** -149 * (terms + 2)
+    if name != "f32":
+        bound = bound * (1 + fi.eps) + fi.eps / 2 * np.abs(want) + fi.smallest_normal * fi.eps / 2
+    bad = ~(np.abs(f64(got) - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), f64(got)[bad][:4], want[bad][:4], np.broadcast_to(bound, want.shape)[bad][:4])
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", [(3, 5, 8), (70, 40, 64), (200, 130, 66)])
+def test_gradients_of_sums_whose_terms_cancel(B, name, M, K, N):
+    """Pairs of terms that differ by a few units of 2^-12 of themselves and have opposite signs: what is left of the sum keeps the type's bits."""
+    rng = np.random.default_rng(M + N)
+    # dx: pairs of channels with the same codes and nearly the same scale
+    w, s_w = np.repeat(codes(rng, N // 2, K), 2, axis=0), np.repeat(scales(rng, N // 2), 2)
+    s_w[1::2] *= (1 + rng.integers(1, 9, N // 2) * 2.0 ** -12).astype(np.float32)
+    dy = np.repeat(rng.standard_normal((M, N // 2)), 2, axis=1) * np.where(np.arange(N) % 2, -1.0, 1.0)
+    t = rounded(dy.astype(np.float32), name)
+    dy = t.float().numpy()
+    a, s_a = codes(rng, M, K), scales(rng, M)
+    dx, _, _ = B.adapt_int8_linear_backward(t.cuda(), dev(a), dev(s_a), dev(w), dev(s_w))
+    (wx, mx), _, _ = ot.int8_linear_backward(dy, a, s_a, w, s_w)
+    within_22_bits(dx, wx, mx, N, name, far_below(dy * s_w, w))
+    # dw: the same with pairs of tokens (the product's two sides change places)
+    _, dw, _ = B.adapt_int8_linear_backward(dev(dy.T).to(_t(name)), dev(w), dev(s_w), dev(a), dev(s_a))
+    _, (ww, mw), _ = ot.int8_linear_backward(dy.T, w, s_w, a, s_a)
+    within_22_bits(dw, ww, mw, N, name, far_below((dy.T * s_w[:, None]).T, w))
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_gradients_keep_what_two_terms_leave(B, name):
+    """(1 + 2^-13) - 1"""
+    near, one = np.array([1 + 2.0 ** -13, 1], np.float32), np.ones(1, np.float32)
+    q1, q2 = np.ones((1, 1), np.int8), np.ones((2, 1), np.int8)
+    dy = dev(np.array([[1, -1]], np.float32)).to(_t(name))
+    dx, _, _ = B.adapt_int8_linear_backward(dy, dev(q1), dev(one), dev(q2), dev(near))
+    _, dw, _ = B.adapt_int8_linear_backward(dy.t().contiguous(), dev(q2), dev(near), dev(q1), dev(one))
+    assert f64(dx) == 2.0 ** -13 and f64(dw) == 2.0 ** -13
