@@ -519,8 +519,8 @@ int adapt_sgd_step_f32(float *w_dev, const float *g_dev, size_t n, float lr, voi
  * Token-wise operators: the exact 8-bit product that a table product is measured against, with a scale for every token and
  * every output channel, its gradients, and the two layers around a recurrent text network that are no products: the
  * embedding and dropout.  Activations and gradients come in the element type the call names (ADAPT_F32, ADAPT_F16,
- * ADAPT_BF16), aligned to their elements; every sum and every step is held in 32 bits (integers, fp32) and rounded to
- * the element type once, to nearest even.  Where a result is a sum of floats its order depends on the sizes alone: the same
+ * ADAPT_BF16), aligned to their elements; every sum and every step is held in 32 bits (integers, fp32; the terms of the product's gradients
+ * in 22, see there) and rounded to the element type once, to nearest even.  Where a result is a sum of floats its order depends on the sizes alone: the same
  * call gives the same bits.  All calls are asynchronous on `stream`, allocate nothing and may be recorded into a HIP
  * graph; what they need beyond operands and results is a workspace of the caller's (aligned to 256 bytes, contents undefined
  * afterwards, not shared by calls that may overlap in time).  Errors: ADAPT_ERR_INVALID_ARGUMENT (NULL or misaligned pointer, unknown
@@ -552,8 +552,8 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
  *     db[n]    = sum_m dy[m][n]
  * dy_dev [M][N], dx_dev [M][K], dw_dev [N][K], db_dev [N] of element type `type`; codes and scales as in adapt_int8_linear.  Any of dx_dev,
  * dw_dev, db_dev may be NULL (not computed; a_dev and s_a_dev are read for dw alone, w_dev and s_w_dev for dx alone).  They are
- * fully overwritten.  dy * s is formed in fp32 and kept to 22 bits, elements far below the largest of their sum's to 2^-40 of that largest; sums are
- * fp32.
+ * fully overwritten.  dy * s is formed in fp32 and kept to 22 bits; an element of it below 2^-17 of the largest in its sum loses 2^-39 of that
+ * largest at most.  Sums are fp32.
  * M, K and N are at most 2^21 and no matrix has 2^34 elements, else ADAPT_ERR_UNSUPPORTED.
  * workspace_dev: the number of bytes that adapt_int8_linear_backward_workspace reports for the same sizes (want_dx / want_dw: whether
  * dx_dev / dw_dev are given; what is reported for both is enough for one).  A gradient has the same bits whatever else is asked for. */

@@ -4,9 +4,9 @@
 //
 // Both are c[i][j] = sum_r t[i][r] q[j][r] with codes q, which are fp16 numbers.  t = dy s becomes fp16 numbers as well: every row i is brought to
 // a largest element in [2^14, 2^15) by a power of two, which goes back in on the sums, and is then the sum of two fp16 numbers, t = t0 + t1, t1 the
-// rest that t0 leaves: 22 bits, 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at every addition.  Elements below 2^-18 of their row's
-// largest keep fewer bits; what they lose is below 2^-40 of that largest.  So a gradient is an fp16 product with exact partial products and fp32 sums over
-// rows [t1 | t0] that meet the same codes twice, the small pieces first.  (One piece of 11 bits is half the work, 288 us against 508 for 4096^3 bf16, but
+// rest that t0 leaves: 22 bits, 2^-22 of a term, where an fp32 sum rounds by 2^-24 of itself at every addition.  Elements below 2^-17 of their row's
+// largest (2^-3 against 2^14) may keep fewer bits: t1 is then off by half the smallest fp16 number, 2^-25, at most 2^-39 of that largest.  So a gradient is an
+// fp16 product with exact partial products and fp32 sums over rows [t1 | t0] that meet the same codes twice, the small pieces first.  (One piece of 11 bits is half the work, 288 us against 508 for 4096^3 bf16, but
 // leaves a bf16 gradient none of its 8 bits where the terms of a sum cancel to 2^-12 of themselves.  Three bf16 pieces of 24 bits, without the rows'
 // powers of two, took 148 us where this takes 114 for 6400 x 512 -> 2048 fp32.)
 //

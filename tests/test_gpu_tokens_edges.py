@@ -1,14 +1,20 @@
-"""Token-wise operators where their definition is easiest to miss: sums whose terms cancel."""
+"""Token-wise operators where their definition is easiest to miss: sums whose terms cancel, elements far below their row's largest."""
 import numpy as np
 import pytest
 
 from oracle import tokens as ot
-from test_gpu_tokens import TYPES, U, B, _t, codes, dev, f64, far_below, rounded, scales  # noqa: F401  (B: the fixture)
+from test_gpu_tokens import TYPES, U, B, _t, codes, dev, f64, rounded, scales  # noqa: F401  (B: the fixture)
 
 pytestmark = pytest.mark.gpu
 
 
 # ---------------------------------------------------------------------------------------------- gradients of the product
+
+def far_below(t, q):
+    """What elements far below the largest of their row t[i] may lose in all: 2^-39 of it for every unit of the codes q [r][j].  (The largest is brought to
+    2^14 at least, and half of the smallest fp16 number is 2^-25.)"""
+    return 2.0 ** -39 * np.abs(t.astype(np.float64)).max(axis=1, initial=0.0)[:, None] * np.abs(q.astype(np.float64)).sum(axis=0)[None, :]
+
 
 def within_22_bits(got, want, mass, terms, name, lost):
     """A gradient of any type: dy * s to 22 bits (2^-22 of a term), sums of fp32, one rounding to the type at the end.  mass: sum of |terms|."""
@@ -51,3 +57,22 @@ def test_gradients_keep_what_two_terms_leave(B, name):
     dx, _, _ = B.adapt_int8_linear_backward(dy, dev(q1), dev(one), dev(q2), dev(near))
     _, dw, _ = B.adapt_int8_linear_backward(dy.t().contiguous(), dev(q2), dev(near), dev(q1), dev(one))
     assert f64(dx) == 2.0 ** -13 and f64(dw) == 2.0 ** -13
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("far", [1.0, 1.5, 2.0, 3.0, 2.0 ** 10])
+@pytest.mark.parametrize("largest", [1.0, 1.9921875])
+def test_gradients_lose_at_most_2_to_minus_39_of_the_largest(B, name, far, largest):
+    """An element of far * 2^-39 beside the largest, which meets a code of 0.  With a largest of a power of two and far = 1 all of it is lost: no
+    smaller bound holds."""
+    small = 1.0 if name == "f16" else 2.0 ** -39            # (fp16 has no 2^-39: the scales bring the elements apart)
+    scale = np.array([1.0, 2.0 ** -39 / small], np.float32)
+    dy = dev(np.array([[largest, far * small]], np.float32)).to(_t(name))
+    q, one = np.array([[0], [1]], np.int8), np.ones(1, np.float32)
+    dx, _, _ = B.adapt_int8_linear_backward(dy, dev(q[:1]), dev(one), dev(q), dev(scale))
+    _, dw, _ = B.adapt_int8_linear_backward(dy.t().contiguous(), dev(q), dev(scale), dev(q[:1]), dev(one))
+    lost = far * 2.0 ** -39 - np.array([f64(dx).item(), f64(dw).item()])
+    step = 2.0 ** -24 if name == "f16" else 0.0             # (nor has its result)
+    assert (np.abs(lost) <= 2.0 ** -39 * largest + step / 2).all()
+    if far == 1 and largest == 1:
+        assert (lost == 2.0 ** -39).all()
