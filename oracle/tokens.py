@@ -7,7 +7,8 @@ import numpy as np
 
 
 def quantize_tokens(x, bits):
-    """x float [M][K] -> (int8 codes, fp32 scales): the scale a product with the rounded 1 / Q, every code by an IEEE fp32 division."""
+    """x float [M][K] -> (int8 codes, fp32 scales): the scale a product with the rounded 1 / Q (tests/test_tokens_definitions_host.py: how far that is
+    from max / Q), every code by an IEEE fp32 division."""
     x = np.asarray(x, dtype=np.float32)
     q_max = np.float32((1 << (bits - 1)) - 1)
     mag = np.where(np.isnan(x), np.float32(0), np.abs(x))

@@ -1,5 +1,7 @@
 // Activations to int8 codes with one scale for each row ("token"): the quantiser of Sec. III-A with the range taken from the row
 // itself.  s = max |x| * (1 / Q), q = clamp(rint(x / s), -Q, Q), every step in fp32; a row of zeros has s = 0 and codes 0.
+// (1 / Q rounded to fp32: within one unit in the last place of max |x| / Q.  Dividing a tensor by a number is this product in torch on the GPU, whose codes
+// these are.)
 #pragma once
 #include "element.hpp"
 #include "elementwise.hpp"
