@@ -520,8 +520,9 @@ int adapt_sgd_step_f32(float *w_dev, const float *g_dev, size_t n, float lr, voi
  * every output channel, its gradients, and the two layers around a recurrent text network that are no products: the
  * embedding and dropout.  Activations and gradients come in the element type the call names (ADAPT_F32, ADAPT_F16,
  * ADAPT_BF16), aligned to their elements; every sum and every step is held in 32 bits (integers, fp32; the terms of the product's gradients
- * in 22, see there) and rounded to the element type once, to nearest even.  Where a result is a sum of floats its order depends on the sizes alone: the same
- * call gives the same bits.  All calls are asynchronous on `stream`, allocate nothing and may be recorded into a HIP
+ * in 22, see there) and rounded to the element type once, to nearest even.  No sum of floats depends on the order in which workgroups run: the same call
+ * on the same kind of device gives the same bits.  (The order goes by the sizes, the number of compute units and, in the embedding's
+ * gradient, by where the places of a token lie among the sorted ones.)  All calls are asynchronous on `stream`, allocate nothing and may be recorded into a HIP
  * graph; what they need beyond operands and results is a workspace of the caller's (aligned to 256 bytes, contents undefined
  * afterwards, not shared by calls that may overlap in time).  Errors: ADAPT_ERR_INVALID_ARGUMENT (NULL or misaligned pointer, unknown
  * element type, negative size, a result that is an operand, workspace too small or misaligned), ADAPT_ERR_UNSUPPORTED (the limits stated),
