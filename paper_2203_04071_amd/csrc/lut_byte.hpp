@@ -477,18 +477,18 @@ __global__ __launch_bounds__(BYTE_THREADS) void lut_byte_kernel(const ByteParams
         const int ns = nsteps;              // (named here: asm operands inside the branches below do not capture)
 #define BYTE_COPY_OP "s_mov_b64 %[sv], exec\n\ts_mov_b64 exec, %[mk]\n\ts_mov_b32 m0, %[to]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[vo], %[sa]\n\ts_mov_b64 exec, %[sv]\n\t"
         if constexpr (FIRST)
-            asm volatile(BYTE_COPY_OP : [sv] "=&s"(save) : [vo] "v"(dma_voff), [mk] "s"(dma_mask), [sa] "s"(src), [to] "s"(to) : "memory");
+            asm volatile(BYTE_COPY_OP : [sv] "=&s"(save) : [vo] "v"(dma_voff), [mk] "s"(dma_mask), [sa] "s"(src), [to] "s"(to) : "memory", "m0");
         else if constexpr (DEEP)
             asm volatile("s_cmp_lt_i32 %[st], %[ns]\n\ts_cbranch_scc0 .Lbyte_none%=\n\t" BYTE_COPY_OP
                          "s_branch .Lbyte_done%=\n.Lbyte_none%=:\n\tglobal_load_dword %[sk], %[vo], %[tb]\n.Lbyte_done%=:"
                          : [sv] "=&s"(save), [sk] "+v"(sink)
                          : [vo] "v"(dma_voff), [tb] "s"(dt), [mk] "s"(dma_mask), [st] "s"(step), [ns] "s"(ns), [sa] "s"(src), [to] "s"(to)
-                         : "memory", "scc");
+                         : "memory", "scc", "m0");
         else
             asm volatile("s_cmp_lt_i32 %[st], %[ns]\n\ts_cbranch_scc0 .Lbyte_done%=\n\t" BYTE_COPY_OP ".Lbyte_done%=:"
                          : [sv] "=&s"(save)
                          : [vo] "v"(dma_voff), [mk] "s"(dma_mask), [st] "s"(step), [ns] "s"(ns), [sa] "s"(src), [to] "s"(to)
-                         : "memory", "scc");
+                         : "memory", "scc", "m0");
 #undef BYTE_COPY_OP
     };
     auto dma_all = [&](int step, int buf, auto first_c, uint32_t &sink) {

@@ -265,7 +265,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const typena
         };
         auto dma1 = [&](int q, int buf) {
             const uint32_t to = lds0 + (uint32_t)(buf * STAGE + place(q));
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(voff[q]), "s"(q < QA ? da : db) : "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(voff[q]), "s"(q < QA ? da : db) : "memory", "m0");
         };
         auto dma_end = [&]() {
             da += SB;
