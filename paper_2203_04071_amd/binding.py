@@ -860,6 +860,12 @@ def _element(dtype):
     return e
 
 
+def _ints(*sizes):
+    """Sizes that the C call takes as int: ctypes would pass on their low 32 bits."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise ValueError(f"a size of {max(sizes)} is above 2147483647")
+
+
 def _arg(what, t, dtype, shape, here):
     """The tensor's address, if it is what the call needs: the library launches on the current device and takes dense rows.  (One test
     of everything: a call's arguments took half as long to check as the launch itself.)"""
@@ -922,6 +928,7 @@ def adapt_int8_linear(a, s_a, w, s_w, bias=None, act: int = 0, dtype=torch.float
     """Codes a [M][K], w [N][K] with scales s_a [M], s_w [N] -> act(a w^T s_a s_w + bias) [M][N] of `dtype` (out's, if given)."""
     M, K = a.shape
     N = w.shape[0]
+    _ints(M, K, N)
     here = _here()
     pa = _arg("a", a, torch.int8, (M, K), here)
     if out is not None:
@@ -939,6 +946,7 @@ def adapt_int8_linear_backward(dy, a, s_a, w, s_w, want=("dx", "dw", "db"), work
     workspace: a uint8 device tensor to reuse (allocated here when None or too small)."""
     M, N = dy.shape
     K = w.shape[1]
+    _ints(M, K, N)
     here = _here()
     e = _element(dy.dtype)
     operands = (_arg("a", a, torch.int8, (M, K), here), _arg("s_a", s_a, torch.float32, (M,), here),
@@ -965,6 +973,7 @@ def _tokens(tokens, here):
 def adapt_embedding(table, tokens, scale: float = 1.0, out=None, stream=None):
     """Rows of table [V][D] for tokens of any shape, times scale; a token outside [0, V) gives zeros."""
     V, D = table.shape
+    _ints(V, D)
     here = _here()
     tok, tok_bits = _tokens(tokens, here)
     pt = _arg("table", table, table.dtype, (V, D), here)
@@ -979,6 +988,7 @@ def adapt_embedding_backward(dy, tokens, V: int, scale: float = 1.0, padding_idx
     """dy [...][D] at tokens [...] -> gradient [V][D] of the table, of dy's type.
     workspace: a uint8 device tensor to reuse (allocated here when None or too small)."""
     D = dy.shape[-1]
+    _ints(V, D)
     here = _here()
     tok, tok_bits = _tokens(tokens, here)
     pdy = _arg("dy", dy, dy.dtype, (*tokens.shape, D), here)

@@ -31,3 +31,32 @@ def test_token_codes_are_those_of_the_quotient_or_one_beside(bits):
     assert np.abs(q.astype(int) - want).max() <= 1
     # the scales differ by 2^-23 of themselves at most, each quotient is rounded once: 3 * 2^-24 of up to Q
     assert (np.abs(np.abs(r[moved]) % 1 - 0.5) <= 3 * 2.0 ** -23 * q_max).all()
+
+
+# ---------------------------------------------------------------------------------------------- the binding
+
+def test_sizes_that_the_library_takes_as_int_are_not_cut():
+    """2^32 + 5 rows are not 5 rows.  (Tensors of no elements, so that the sizes are all there is; refused before the device is touched.)"""
+    import torch
+
+    from paper_2203_04071_amd import binding as B
+    far = (1 << 32) + 5
+    q = lambda *s: torch.empty(s, dtype=torch.int8)
+    f = torch.empty
+    big = "above 2147483647"
+    for a, w in ((q(far, 0), q(3, 0)), (q(3, 0), q(far, 0)), (q(0, far), q(0, far)), (q((1 << 31), 0), q(3, 0))):
+        M, N = a.shape[0], w.shape[0]
+        with pytest.raises(ValueError, match=big):
+            B.adapt_int8_linear(a, f(0), w, f(0))
+        if not M * N:
+            with pytest.raises(ValueError, match=big):
+                B.adapt_int8_linear_backward(f(M, N), a, f(0), w, f(0))
+    for M, N in ((far, 0), (0, far)):
+        with pytest.raises(ValueError, match=big):
+            B.adapt_int8_linear_backward(f(M, N), q(M, 0), f(0), q(N, 0), f(0))
+    none = torch.empty(0, dtype=torch.int64)
+    for V, D in ((far, 0), (0, far)):
+        with pytest.raises(ValueError, match=big):
+            B.adapt_embedding(f(V, D), none)
+        with pytest.raises(ValueError, match=big):
+            B.adapt_embedding_backward(f(0, D), none, V)
