@@ -544,8 +544,8 @@ int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *s
  *     acc[m][n] = sum_k a[m][k] * w[n][k]   (int32, exact: the sums of adapt_approx_linear with the table of the exact product)
  *     y[m][n] = float(acc) * s_a[m] * s_w[n], then + bias[n] if bias_dev, then act (0 none, 1 y > 0 ? y : 0, 2 adapt_tanh_f32)
  * left to right, every fp32 step rounded on its own.  a_dev [M][K], w_dev [N][K] int8; s_a_dev [M], s_w_dev [N], bias_dev [N]
- * fp32; y_dev [M][N] of type y_type.  K = 0: sums of 0.  K <= 131071 (beyond, a sum may pass 32 bits) and M N < 2^36, else
- * ADAPT_ERR_UNSUPPORTED. */
+ * fp32; y_dev [M][N] of type y_type.  K = 0: sums of 0.  K <= 131071 (beyond, a sum may pass 32 bits) and fewer than 2^24 blocks of 64 x 64
+ * outputs, begun ones included (2^36 outputs of many rows and channels, 2^30 - 64 channels of up to 64 rows), else ADAPT_ERR_UNSUPPORTED. */
 int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w_dev, const float *s_w_dev, const float *bias_dev, int act,
                       void *y_dev, int y_type, int M, int K, int N, void *stream);
 

@@ -322,7 +322,7 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
     for (const void *q : {(const void *)a_dev, (const void *)w_dev, (const void *)s_a_dev, (const void *)s_w_dev, (const void *)bias_dev})
         if (q == y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
     if (K > INT8_MAX_K) return fail(ADAPT_ERR_UNSUPPORTED, "%s: K=%d above %d, sums could pass 32 bits", who, K, INT8_MAX_K);
-    if ((((long long)M + 63) / 64) * (((long long)N + 63) / 64) >= MAX_TILES) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^36 outputs or more", who);
+    if ((((long long)M + 63) / 64) * (((long long)N + 63) / 64) >= MAX_TILES) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^24 blocks of 64 x 64 outputs or more", who);
     const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, bias_dev, y_dev, M, K, N, act};
     ADAPT_FOR_TYPE(y_type, E, launch_int8<E>(p, (hipStream_t)stream));
     HIP_TRY(hipGetLastError());

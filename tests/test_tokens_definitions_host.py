@@ -60,3 +60,14 @@ def test_sizes_that_the_library_takes_as_int_are_not_cut():
             B.adapt_embedding(f(V, D), none)
         with pytest.raises(ValueError, match=big):
             B.adapt_embedding_backward(f(0, D), none, V)
+
+
+def test_product_of_too_many_blocks_is_refused_for_that():
+    """The limit counts blocks of 64 x 64 outputs: one row of 2^30 channels is refused, as is 2^18 x 2^18, and told so."""
+    import ctypes
+
+    from paper_2203_04071_amd import binding as B
+    L, p = B.load(), ctypes.c_void_p(256)
+    for M, N in ((1, 1 << 30), (64, (1 << 30) - 63), ((1 << 30) - 63, 1), ((1 << 31) - 1, (1 << 31) - 1), (1 << 18, 1 << 18), ((1 << 18) - 63, (1 << 18) - 63)):
+        assert L.adapt_int8_linear(p, p, p, p, None, 0, ctypes.c_void_p(512), 0, M, 4, N, None) == -2
+        assert "2^24 blocks of 64 x 64 outputs" in L.adapt_last_error().decode()
