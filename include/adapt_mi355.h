@@ -525,7 +525,7 @@ int adapt_sgd_step_f32(float *w_dev, const float *g_dev, size_t n, float lr, voi
  * gradient, by where the places of a token lie among the sorted ones.)  All calls are asynchronous on `stream`, allocate nothing and may be recorded into a HIP
  * graph; what they need beyond operands and results is a workspace of the caller's (aligned to 256 bytes, contents undefined
  * afterwards, not shared by calls that may overlap in time).  Errors: ADAPT_ERR_INVALID_ARGUMENT (NULL or misaligned pointer, unknown
- * element type, negative size, a result that is an operand, workspace too small or misaligned), ADAPT_ERR_UNSUPPORTED (the limits stated),
+ * element type, negative size, a result or workspace that is an operand or another result, workspace too small or misaligned), ADAPT_ERR_UNSUPPORTED (the limits stated),
  * ADAPT_ERR_HIP.
  * ---------------------------------------------------------------------------------------------- */
 

@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -34,6 +35,12 @@ inline int fail(int code, const char *fmt, ...) {
             return fail(e_ == hipErrorOutOfMemory ? ADAPT_ERR_OUT_OF_MEMORY : ADAPT_ERR_HIP, "%s: %s", \
                         #expr, hipGetErrorString(e_));                                                 \
     } while (0)
+
+inline bool is_one_of(const void *p, std::initializer_list<const void *> others) {      // (nullptr is none)
+    for (const void *q : others)
+        if (p && p == q) return true;
+    return false;
+}
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

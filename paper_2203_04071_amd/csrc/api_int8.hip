@@ -319,8 +319,7 @@ int adapt_int8_linear(const int8_t *a_dev, const float *s_a_dev, const int8_t *w
     if (!s_a_dev || !s_w_dev || !y_dev || (K && (!a_dev || !w_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
     if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4) || off_by(bias_dev, 4) || off_by(y_dev, (size_t)adapt::element_size(y_type)))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    for (const void *q : {(const void *)a_dev, (const void *)w_dev, (const void *)s_a_dev, (const void *)s_w_dev, (const void *)bias_dev})
-        if (q == y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
+    if (is_one_of(y_dev, {a_dev, w_dev, s_a_dev, s_w_dev, bias_dev})) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
     if (K > INT8_MAX_K) return fail(ADAPT_ERR_UNSUPPORTED, "%s: K=%d above %d, sums could pass 32 bits", who, K, INT8_MAX_K);
     if ((((long long)M + 63) / 64) * (((long long)N + 63) / 64) >= MAX_TILES) return fail(ADAPT_ERR_UNSUPPORTED, "%s: 2^24 blocks of 64 x 64 outputs or more", who);
     const adapt::Int8Params p{a_dev, w_dev, s_a_dev, s_w_dev, bias_dev, y_dev, M, K, N, act};
@@ -352,9 +351,11 @@ int adapt_int8_linear_backward(const void *dy_dev, int type, const int8_t *a_dev
     for (const void *q : {dy_dev, (const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
         if (off_by(q, e)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
     if (off_by(s_a_dev, 4) || off_by(s_w_dev, 4)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    for (const void *g : {(const void *)dx_dev, (const void *)dw_dev, (const void *)db_dev})
-        if (g && (g == dy_dev || g == (const void *)a_dev || g == (const void *)w_dev))
-            return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
+    for (const void *g : {dx_dev, dw_dev, db_dev})
+        if (is_one_of(g, {dy_dev, a_dev, w_dev, s_a_dev, s_w_dev})) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: a gradient must not alias an input", who);
+    if (is_one_of(dx_dev, {dw_dev, db_dev}) || is_one_of(dw_dev, {db_dev})) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: gradients must not alias each other", who);
+    if (is_one_of(workspace_dev, {dy_dev, a_dev, w_dev, s_a_dev, s_w_dev, dx_dev, dw_dev, db_dev}))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: the workspace must not alias an operand or a gradient", who);
     if (int rc = grad_limits(who, M, K, N)) return rc;
     const GradPlans plans = grad_plans(M, K, N, want_dx, want_dw);
     const size_t need = plans.bytes;

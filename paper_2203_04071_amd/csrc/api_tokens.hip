@@ -117,6 +117,7 @@ int dropout(const char *who, const void *x_dev, void *y_dev, int type, size_t n,
     if (!n) return ADAPT_OK;
     if (!x_dev || !y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
     if (off_by(x_dev, e) || off_by(y_dev, e) || off_by(step_dev, 8)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
+    if (is_one_of(y_dev, {step_dev})) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: the result must not be the step", who);
     adapt::DropoutParams q{};
     q.seed = seed;
     q.offset = offset;
@@ -146,7 +147,7 @@ int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *s
     if (!tokens) return ADAPT_OK;
     if (!scales_dev || (cols && (!x_dev || !q_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
     if (off_by(x_dev, e) || off_by(scales_dev, 4)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    if (cols && x_dev == (const void *)q_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
+    if (cols && (is_one_of(x_dev, {q_dev, scales_dev}) || is_one_of(q_dev, {scales_dev}))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
     const float Q = (float)((1 << (bits - 1)) - 1);
     ADAPT_FOR_TYPE(x_type, E, quantize_tokens<E>(static_cast<const E::mem *>(x_dev), q_dev, scales_dev, tokens, cols, Q, (hipStream_t)stream));
     HIP_TRY(hipGetLastError());
@@ -166,7 +167,7 @@ int adapt_embedding(const void *table_dev, int type, const void *tokens_dev, int
     if (!tokens_dev || !y_dev || (V && !table_dev)) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
     if (off_by(table_dev, e) || off_by(y_dev, e) || off_by(tokens_dev, (size_t)token_bits / 8))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    if (table_dev == y_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
+    if (is_one_of(y_dev, {table_dev, tokens_dev})) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: in-place not possible", who);
     hipStream_t s = (hipStream_t)stream;
     ADAPT_FOR_TYPE(type, E, {
         const int lg = lanes_lg<E>(D);
@@ -205,7 +206,9 @@ int adapt_embedding_backward(const void *dy_dev, int type, const void *tokens_de
     if (!dtable_dev || (tokens && (!tokens_dev || !dy_dev))) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: NULL pointer", who);
     if (off_by(dy_dev, e) || off_by(dtable_dev, e) || off_by(tokens_dev, (size_t)token_bits / 8))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: pointer not aligned to its elements", who);
-    if (dy_dev == dtable_dev) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: the gradient must not alias an input", who);
+    if (is_one_of(dtable_dev, {dy_dev, tokens_dev})) return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: the gradient must not alias an input", who);
+    if (is_one_of(workspace_dev, {dy_dev, tokens_dev, dtable_dev}))
+        return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: the workspace must not alias an operand or the gradient", who);
     const EmbedPlan pl = embed_plan(tokens, V, D);
     if (!workspace_dev || workspace_bytes < pl.bytes || off_by(workspace_dev, 256))
         return fail(ADAPT_ERR_INVALID_ARGUMENT, "%s: workspace of %zu bytes, aligned to 256, is needed", who, pl.bytes);

@@ -71,3 +71,37 @@ def test_product_of_too_many_blocks_is_refused_for_that():
     for M, N in ((1, 1 << 30), (64, (1 << 30) - 63), ((1 << 30) - 63, 1), ((1 << 31) - 1, (1 << 31) - 1), (1 << 18, 1 << 18), ((1 << 18) - 63, (1 << 18) - 63)):
         assert L.adapt_int8_linear(p, p, p, p, None, 0, ctypes.c_void_p(512), 0, M, 4, N, None) == -2
         assert "2^24 blocks of 64 x 64 outputs" in L.adapt_last_error().decode()
+
+
+# ---------------------------------------------------------------------------------------------- results that are operands
+
+def test_results_and_workspaces_that_are_operands_or_other_results_are_refused():
+    import ctypes
+
+    from paper_2203_04071_amd import binding as B
+    L, vp, n = B.load(), ctypes.c_void_p, ctypes.c_size_t()
+
+    def refused(call, good, pairs):
+        for a, b in pairs:
+            args = dict(good)
+            args[a] = args[b]
+            assert call(*args.values()) == -1, (a, b)
+            text = L.adapt_last_error().decode()
+            assert "alias" in text or "in-place" in text or "step" in text, (a, b, text)
+
+    refused(L.adapt_quantize_tokens, dict(x=vp(256), type=0, q=vp(512), scales=vp(768), tokens=4, cols=8, bits=8, stream=None),
+            (("q", "x"), ("scales", "x"), ("scales", "q")))
+    refused(L.adapt_int8_linear, dict(a=vp(256), s_a=vp(512), w=vp(768), s_w=vp(1024), bias=vp(1280), act=0, y=vp(1536), type=0, M=4, K=8, N=4, stream=None),
+            [("y", b) for b in ("a", "s_a", "w", "s_w", "bias")])
+    assert L.adapt_int8_linear_backward_workspace(64, 48, 32, 0, 1, 1, ctypes.byref(n)) == 0
+    operands, results = ("dy", "a", "s_a", "w", "s_w"), ("dx", "dw", "db")
+    refused(L.adapt_int8_linear_backward, dict(dy=vp(256), type=0, a=vp(512), s_a=vp(768), w=vp(1024), s_w=vp(1280), M=64, K=48, N=32, dx=vp(2048),
+                                               dw=vp(4096), db=vp(8192), ws=vp(1 << 20), n=n.value, stream=None),
+            [(r, o) for r in results + ("ws",) for o in operands] + [("dw", "dx"), ("db", "dx"), ("db", "dw")] + [("ws", r) for r in results])
+    refused(L.adapt_embedding, dict(table=vp(256), type=0, tok=vp(512), bits=64, y=vp(1024), T=4, V=8, D=16, scale=1.0, stream=None),
+            (("y", "table"), ("y", "tok")))
+    assert L.adapt_embedding_backward_workspace(4, 8, 16, ctypes.byref(n)) == 0
+    refused(L.adapt_embedding_backward, dict(dy=vp(256), type=0, tok=vp(512), bits=64, out=vp(1024), T=4, V=8, D=16, scale=1.0, pad=-1, ws=vp(4096), n=n.value, stream=None),
+            [(r, o) for r in ("out", "ws") for o in ("dy", "tok")] + [("ws", "out")])
+    for call in (L.adapt_dropout, L.adapt_dropout_backward):
+        refused(call, dict(x=vp(256), y=vp(512), type=0, n=4, p=0.5, seed=1, offset=0, step=vp(1024), stream=None), (("y", "step"),))
