@@ -256,7 +256,7 @@ __global__ __launch_bounds__(TILE_THREADS) void tile_product_kernel(const typena
     if constexpr (DMA) {
         int dma_s = 0;          // stage that is requested next
         const int Kb_b = p.Kb_b;        // (a copy: the parameters of a pair would be read again in every stage)
-        int kb = Op::INT ? 0 : k0 % Kb_b;
+        int kb = Op::INT || total == 0 ? 0 : k0 % Kb_b;        // (no sums: no rows of b either)
         const char *da = abase, *db = bbase + kb;
         auto dma_begin = [&]() {        // where the last stage is not whole, lanes whose piece lies behind the end fetch its first piece instead
             if (Op::INT && dma_s == full && piece16 >= rest)

@@ -76,3 +76,20 @@ def test_gradients_lose_at_most_2_to_minus_39_of_the_largest(B, name, far, large
     assert (np.abs(lost) <= 2.0 ** -39 * largest + step / 2).all()
     if far == 1 and largest == 1:
         assert (lost == 2.0 ** -39).all()
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", [(0, 8, 9), (7, 300, 0), (5, 0, 6), (0, 1000, 300), (600, 130, 0)])
+def test_gradients_of_empty_sums(B, name, M, K, N):
+    """No tokens: dw and db are zeros; no channels: dx is; whatever the results' memory held before."""
+    import torch
+    z = lambda *s: torch.zeros(s, dtype=torch.int8, device="cuda")
+    for want in (("dx", "dw", "db"), ("dx",), ("dw",), ("db",)):
+        for _ in range(2):
+            junk = [torch.full((n,), float("nan"), dtype=_t(name), device="cuda") for n in (M * K, N * K, N)]
+            del junk
+            dx, dw, db = B.adapt_int8_linear_backward(torch.ones((M, N), dtype=_t(name), device="cuda"), z(M, K), torch.ones(M, device="cuda"), z(N, K),
+                                                      torch.ones(N, device="cuda"), want=want)
+            assert dx is None or (dx.shape == (M, K) and (dx == 0).all())
+            assert dw is None or (dw.shape == (N, K) and (dw == 0).all())
+            assert db is None or (db.shape == (N,) and (db == M).all())
