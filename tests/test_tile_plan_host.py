@@ -22,6 +22,25 @@ PRODUCTS = {
     "64x64 six": [(67, 16, 1452), (66, 80, 1464), (65, 128, 1458), (70, 144, 1426), (67, 336, 1443), (65, 384, 1603)],
 }
 
+# M, K, N of gradients whose two products share a launch: kind, whether dx's and dw's sums are in parts
+JOINT = {
+    ("256x256", False, False): (1564, 3985, 1433), ("256x128", False, False): (516, 3841, 661), ("256x128", False, True): (5095, 1812, 65),
+    ("256x128", True, False): (95, 1914, 4998), ("256x128", True, True): (2960, 133, 5557), ("128x128", False, False): (208, 3271, 324),
+    ("128x128", False, True): (5048, 911, 8), ("128x128", True, False): (8, 827, 5601), ("128x128", True, True): (3151, 69, 2639),
+    ("128x128 two", False, False): (395, 3611, 575), ("128x128 two", False, True): (1251, 2399, 67), ("128x128 two", True, False): (65, 1811, 1705),
+    ("128x64", False, False): (8, 2638, 464), ("128x64", False, True): (4342, 263, 8), ("128x64", True, False): (8, 391, 3025),
+    ("128x64", True, True): (1235, 1, 3370), ("64x64", False, False): (8, 1, 65), ("64x64", False, True): (782, 1, 8), ("64x64", True, False): (8, 1, 770),
+    ("64x64", True, True): (911, 1, 1415), ("64x64 six", False, False): (8, 1, 8), ("64x64 six", False, True): (1127, 2719, 8),
+    ("64x64 six", True, False): (8, 3120, 970),
+}
+
+# ... and of gradients whose products are two launches: dx's kind, in parts or not, dw's
+APART = {
+    ("256x256", False, "128x128", True): (4308, 3808, 206), ("128x128", True, "256x256", False): (257, 2654, 4802), ("256x128", False, "128x128", True): (3853, 1757, 453),
+    ("128x64", False, "128x128", False): (1523, 1127, 2112), ("128x128", True, "128x128 two", False): (68, 3518, 5940), ("128x128 two", False, "128x64", True): (5622, 2820, 72),
+    ("64x64", True, "64x64 six", False): (8, 1852, 2491), ("64x64 six", False, "64x64", True): (4575, 1048, 8), ("64x64", True, "128x128 two", False): (8, 1302, 4864),
+}
+
 PROGRAM = r'''
 #include <cstdio>
 #include "tile_plan.hpp"
@@ -65,3 +84,16 @@ def test_products_take_every_kind_of_tile(plan):
         assert {K % STAGE[kind] == 0 for _, K, _ in sizes} == {False, True}     # a last stage that is whole, one that is not
         tm, tn = (int(v) for v in kind.split()[0].split("x"))
         assert any(M % tm and N % tn for M, _, N in sizes)
+
+
+def test_gradients_take_every_kind_of_tile_in_one_launch(plan):
+    keys = list(JOINT)
+    for key, (_, joint, k0, s0, k1, s1) in zip(keys, plan([JOINT[k] for k in keys])):
+        assert joint and (KINDS[k0], s0 > 1, s1 > 1) == key and k0 == k1
+    assert {k[0] for k in keys} == set(KINDS)
+
+
+def test_gradients_in_two_launches(plan):
+    keys = list(APART)
+    for key, (_, joint, k0, s0, k1, s1) in zip(keys, plan([APART[k] for k in keys])):
+        assert not joint and (KINDS[k0], s0 > 1, KINDS[k1], s1 > 1) == key
