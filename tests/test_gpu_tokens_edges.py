@@ -1,9 +1,9 @@
-"""Token-wise operators where their definition is easiest to miss: sums whose terms cancel, elements far below their row's largest."""
+"""Token-wise operators where their definition is easiest to miss: sums whose terms cancel, elements far below their row's largest, the order of places."""
 import numpy as np
 import pytest
 
 from oracle import tokens as ot
-from test_gpu_tokens import TYPES, U, B, _t, codes, dev, f64, rounded, scales  # noqa: F401  (B: the fixture)
+from test_gpu_tokens import TYPES, U, B, _t, codes, dev, f64, randn, rounded, same_bits, scales, tokens_of, within  # noqa: F401  (B: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +93,24 @@ def test_gradients_of_empty_sums(B, name, M, K, N):
             assert dx is None or (dx.shape == (M, K) and (dx == 0).all())
             assert dw is None or (dw.shape == (N, K) and (dw == 0).all())
             assert db is None or (db.shape == (N,) and (db == M).all())
+
+
+# ---------------------------------------------------------------------------------------------- embedding
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("T,V,D", [(300, 7, 40), (4096, 100, 33), (40000, 50000, 64), (70001, 12, 40)])
+def test_embedding_gradient_does_not_depend_on_where_the_places_lie(B, name, T, V, D):
+    """Tokens in another order, the gradients moved with them so that every token's places keep theirs: the same sums in the same order, the same bits."""
+    rng = np.random.default_rng(T)
+    tok = tokens_of(rng, "zipf", T, V)
+    tok[rng.random(T) < 0.4] = 3
+    dy, dyd = randn(rng, (T, D), name)
+    got = B.adapt_embedding_backward(dyd, dev(tok), V, scale=0.7)
+    want, mass, n = ot.embedding_backward(dy, tok, V, 0.7)
+    within(got, want, mass, n[:, None], name)
+    other = rng.permutation(tok)
+    assert (other != tok).any()
+    moved = np.empty_like(dy)
+    moved[np.argsort(other, kind="stable")] = dy[np.argsort(tok, kind="stable")]
+    assert np.array_equal(moved[other == 3], dy[tok == 3])
+    same_bits(B.adapt_embedding_backward(rounded(moved, name).cuda(), dev(other), V, scale=0.7), got.cpu())
