@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import oracle as orc
 from oracle import tokens as ot
 from test_gpu_tokens import TYPES, U, B, _t, codes, dev, f64, randn, rounded, same_bits, scales, tokens_of, within  # noqa: F401  (B: the fixture)
 
@@ -114,3 +115,18 @@ def test_embedding_gradient_does_not_depend_on_where_the_places_lie(B, name, T, 
     moved[np.argsort(other, kind="stable")] = dy[np.argsort(tok, kind="stable")]
     assert np.array_equal(moved[other == 3], dy[tok == 3])
     same_bits(B.adapt_embedding_backward(rounded(moved, name).cuda(), dev(other), V, scale=0.7), got.cpu())
+
+
+# ---------------------------------------------------------------------------------------------- product
+
+# few tokens; rows of 16-byte pieces; rows of any length (each of them with and without whole stages and whole tiles)
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", [(1, 512, 2048), (16, 304, 70), (7, 301, 70), (16, 3, 17), (17, 512, 64), (40, 304, 70), (300, 1040, 257), (640, 128, 640),
+                                   (17, 15, 64), (40, 300, 70), (300, 513, 130), (2050, 77, 300)])
+def test_product_with_tanh(B, name, M, K, N):
+    rng = np.random.default_rng(M + K)
+    a, w, s_a, s_w = codes(rng, M, K), codes(rng, N, K), scales(rng, M) * 0.1, scales(rng, N) * 0.1
+    bias = rng.standard_normal(N).astype(np.float32)
+    for b in (None, bias):
+        got = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), bias=None if b is None else dev(b), act=2, dtype=_t(name))
+        same_bits(got, rounded(ot.int8_linear(a, s_a, w, s_w, b, 2, tanh=orc.tanh), name))
