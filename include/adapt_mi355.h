@@ -535,8 +535,8 @@ int adapt_sgd_step_f32(float *w_dev, const float *g_dev, size_t n, float lr, voi
  * in fp32 (the codes by IEEE division: those of adapt_quantize_rows_f32 with these scales), 2 <= bits <= 8.  The scale is a product, where the rule for
  * a calibrated range above, amax / Q, is a division: it is that quotient or the fp32 number beside it (the quotient for bits = 2), and a code is that of
  * the quotient's scale or, where x / scale comes as close as that to a half, one beside it.  A program that compares with ranges of its own takes
- * adapt_absmax_rows_f32, forms the scales itself and calls adapt_quantize_rows_f32.  A row that holds an infinity gets scales[t] = inf and codes 0: its products with
- * adapt_int8_linear are NaN.  q_dev [tokens][cols] int8, scales_dev [tokens] fp32. */
+ * adapt_absmax_rows_f32, forms the scales itself and calls adapt_quantize_rows_f32.  A row that holds an infinity gets scales[t] = inf and codes 0:
+ * adapt_int8_linear then gives NaN for that token, or 0 with act = 1, whose comparison NaN fails.  q_dev [tokens][cols] int8, scales_dev [tokens] fp32. */
 int adapt_quantize_tokens(const void *x_dev, int x_type, int8_t *q_dev, float *scales_dev, size_t tokens, size_t cols, int bits,
                           void *stream);
 

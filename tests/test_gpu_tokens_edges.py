@@ -130,3 +130,21 @@ def test_product_with_tanh(B, name, M, K, N):
     for b in (None, bias):
         got = B.adapt_int8_linear(dev(a), dev(s_a), dev(w), dev(s_w), bias=None if b is None else dev(b), act=2, dtype=_t(name))
         same_bits(got, rounded(ot.int8_linear(a, s_a, w, s_w, b, 2, tanh=orc.tanh), name))
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("M,K,N", [(5, 64, 40), (300, 256, 300), (300, 257, 300)])
+def test_tokens_that_hold_an_infinity(B, name, M, K, N):
+    """Their scale is infinite, their codes 0: NaN in every channel, which a ReLU turns into 0.  The other tokens do not see them."""
+    rng = np.random.default_rng(K)
+    x, _ = randn(rng, (M, K), name)
+    x[1, 3], x[4, K - 1] = np.inf, -np.inf
+    a, s_a = B.adapt_quantize_tokens(dev(x).to(_t(name)))
+    w, s_w = codes(rng, N, K), scales(rng, N)
+    q, s = ot.quantize_tokens(x, 8)
+    assert (q[[1, 4]] == 0).all() and np.isinf(s[[1, 4]]).all()
+    for act in (0, 1):
+        got = B.adapt_int8_linear(a, s_a, dev(w), dev(s_w), act=act, dtype=_t(name))
+        same_bits(got, rounded(ot.int8_linear(q, s, w, s_w, None, act), name))
+        rows = f64(got)[[1, 4]]
+        assert np.isnan(rows).all() if act == 0 else (rows == 0).all()
