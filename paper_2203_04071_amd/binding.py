@@ -846,7 +846,8 @@ def adapt_relu_backward_f32(dy, y, out=None, stream=None):
     return out
 
 
-# ---- token-wise operators: element types, and results in memory of the stream the call runs on
+# ---- token-wise operators: element types, and results in memory of the stream the call runs on.  With `stream`, operands of another stream are the
+# caller's to keep (and to have ready) until that stream is done with them, as for any operator of torch.
 
 ELEMENT_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
@@ -885,7 +886,11 @@ def _arg(what, t, dtype, shape, here):
 
 
 def _raw_stream(stream, here):
-    return torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(here)
+    if stream.device.index != here:
+        raise ValueError(f"stream is of cuda:{stream.device.index}, but the current device is cuda:{here}")
+    return stream.cuda_stream
 
 
 def _new(stream, like, shape, dtype):

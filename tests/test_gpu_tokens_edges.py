@@ -148,3 +148,28 @@ def test_tokens_that_hold_an_infinity(B, name, M, K, N):
         same_bits(got, rounded(ot.int8_linear(q, s, w, s_w, None, act), name))
         rows = f64(got)[[1, 4]]
         assert np.isnan(rows).all() if act == 0 else (rows == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------- streams
+
+def test_every_operator_on_a_stream_given_to_the_call(B):
+    """The same results as on the current stream, whose work they wait for by the caller's own event."""
+    import torch
+    rng = np.random.default_rng(4)
+    M, K, N, V = 500, 96, 120, 70
+    a, s_a, w, s_w = dev(codes(rng, M, K)), dev(scales(rng, M)), dev(codes(rng, N, K)), dev(scales(rng, N))
+    _, x = randn(rng, (M, K), "bf16")
+    _, dy = randn(rng, (M, N), "bf16")
+    _, table = randn(rng, (V, K), "bf16")
+    tok = dev(tokens_of(rng, "zipf", M, V))
+    calls = [lambda **k: B.adapt_quantize_tokens(x, **k), lambda **k: (B.adapt_int8_linear(a, s_a, w, s_w, **k),),
+             lambda **k: B.adapt_int8_linear_backward(dy, a, s_a, w, s_w, **k), lambda **k: (B.adapt_embedding(table, tok, **k),),
+             lambda **k: (B.adapt_embedding_backward(x, tok, V, **k),), lambda **k: (B.adapt_dropout(x, 0.5, 1, **k),), lambda **k: (B.adapt_dropout_backward(x, 0.5, 1, **k),)]
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(2):
+        got = [c(stream=s) for c in calls]
+        s.synchronize()
+        for g, v in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(g, v))

@@ -105,3 +105,15 @@ def test_results_and_workspaces_that_are_operands_or_other_results_are_refused()
             [(r, o) for r in ("out", "ws") for o in ("dy", "tok")] + [("ws", "out")])
     for call in (L.adapt_dropout, L.adapt_dropout_backward):
         refused(call, dict(x=vp(256), y=vp(512), type=0, n=4, p=0.5, seed=1, offset=0, step=vp(1024), stream=None), (("y", "step"),))
+
+
+def test_a_stream_of_another_device_is_refused():
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2203_04071_amd import binding as B
+    stream = SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=7)
+    with pytest.raises(ValueError, match="cuda:1"):
+        B._raw_stream(stream, 0)
+    assert B._raw_stream(stream, 1) == 7
