@@ -173,3 +173,16 @@ def test_every_operator_on_a_stream_given_to_the_call(B):
         s.synchronize()
         for g, v in zip(got, want):
             assert all(torch.equal(p, q) for p, q in zip(g, v))
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("V,D", [(1, 1), (5, 7), (1000, 33), (3, 5000)])
+def test_embedding_without_places(B, name, V, D):
+    """No tokens: no rows, and a gradient of zeros whatever its memory held."""
+    import torch
+    for dtype in (torch.int32, torch.int64):
+        tok = torch.empty(0, dtype=dtype, device="cuda")
+        assert B.adapt_embedding(torch.ones((V, D), dtype=_t(name), device="cuda"), tok).shape == (0, D)
+        out = torch.full((V + 1, D), float("nan"), dtype=_t(name), device="cuda")
+        B.adapt_embedding_backward(torch.empty((0, D), dtype=_t(name), device="cuda"), tok, V, out=out[:V])
+        assert (out[:V] == 0).all() and torch.isnan(out[V]).all()
