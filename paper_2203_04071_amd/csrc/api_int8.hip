@@ -89,7 +89,7 @@ void launch_ragged(const adapt::TileParams &p, hipStream_t s) {
 // Few tokens, or few tiles: the kernel without LDS tiles (int8_tokens_kernel) reads 16 (MT + 1) K bytes per workgroup of 16 x 16 MT outputs, at about
 // 13 TB/s from L2; a tile of 64 x 64 takes K / 128 stages of 0.15 us whatever the number of tiles, up to two per compute unit.  They meet where
 // (MT + 1) times the number of workgroups is 900: 32 x 4096 x 4096 8.1 us against 10.4, 64 x 4096 x 4096 11.6 against 10.1, 64 x 8192 -> 256
-// 9.1 against 17, 8 x 4096 -> 16384 17 against 12.6.  Rows that are no multiple of 16 bytes (up to 64 tokens): always.
+// 9.1 against 17, 8 x 4096 -> 16384 17 against 12.  Rows that are no multiple of 16 bytes (up to 64 tokens): always.
 int tokens_kernel_mt(int M, int N, bool dma) {
     const long long n16 = ((long long)N + 15) / 16;
     if (n16 >= TOKENS_GROUPS) return 0;
@@ -131,7 +131,8 @@ void launch_int8(const adapt::Int8Params &q, hipStream_t s) {
     p.act = q.act;
     p.c = q.y;
     const TilePlan small = one_tile(p.I, p.J, p.Kb, 64, 64);
-    if (q.act == 2) {       // (tanh: one kernel for each way of reading)
+    // (tanh: one kernel for each way of reading.  6400 x 512 -> 2048 fp32 35 us where the plain product takes 19, 8192^3 bf16 925 against 477, up to 40 tokens the same)
+    if (q.act == 2) {
         if (q.M <= 16 && q.N <= 16 * (TOKENS_GROUPS - 1)) launch_tokens<E, 1, true>(q, s);
         else if (dma) launch_tile<E, 64, 64, 128, 4, true, true>(p, small, s);
         else launch_tile<E, 64, 64, 64, 2, false, true>(p, small, s);

@@ -12,8 +12,9 @@ struct Int8Params {
 };
 
 // Rows that do not start at multiples of four bytes: a 16-byte request at an odd address takes the memory pipe two to four times as long as one
-// at a multiple of four (1111 x 4095 -> 999: 262 us, so read 107, 4092 74).  So the aligned 16 bytes and the word behind them are requested, and the bytes moved down when they are used.  The last
-// row (the word behind its end may lie outside the matrix), and every row of a matrix that itself is not aligned, is read as it lies.
+// at a multiple of four (8 tokens, 16384 channels of 4095: 48 us; of 4092 16.5).  So the aligned 16 bytes and the word behind them are requested, and the
+// bytes moved down when they are used (30 us; 48 x 3001 -> 4096 17.3 -> 12.4).  The last row (the word behind its end may lie outside the matrix), and every
+// row of a matrix that itself is not aligned, is read as it lies.
 template <bool SHIFT>
 struct RowBytes {
     const char *row;            // of the first request

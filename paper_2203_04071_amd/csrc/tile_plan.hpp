@@ -113,9 +113,11 @@ inline double tile_end(long long n0, double t0, long long n1, double t1, long lo
 }
 
 // Two products, in one launch of one kind of tile or one after the other.  One launch fills the last rounds of both and saves 3 us, but is one
-// kind for two shapes.  1000 x 1000 -> 1000 bf16 (whole gradient) 30.0 -> 26.8 us, 6400 x 512 -> 2048 fp32 124 -> 117, 100000 x 512 -> 512 fp32 628 -> 519
-// (most of it from more parts).  Above 40 us estimates decide by more than their error only: 40 x 3408 -> 16176 bf16, estimated 4 % longer in one
-// launch, took 119 us against 103.
+// kind for two shapes.  Whole gradients in two launches and in one: 1000 x 1000 -> 1000 bf16 39.4 and 30.6 us, 6400 x 512 -> 2048 fp32 119.7 and 115.3, 3386 x 3066
+// -> 408 bf16 90 and 68, 55 x 14134 -> 16177 fp32 593 and 641, 41 x 12179 -> 12837 bf16 366 and 390, 76 x 8301 -> 7271 bf16 170 and 155.  Above 40 us estimates
+// decide by 2 % only; over 36 drawn gradients the plan is 0.5 % slower than one launch for all and 9 % faster than two (one of the last three sizes
+// goes the wrong way).  The estimates are made for int8 products: those of fp16 numbers come out a quarter too short (6400 x 512 -> 2048 fp32 44 us,
+// measured 60), which both sides of the comparison share.
 struct TilePairPlan {
     TilePlan plan[2];
     bool joint;
